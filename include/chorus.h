@@ -23,7 +23,12 @@
  *   - block-pair visit refreshing over a layer group (Sec. 3.2 "Safety
  *     fallback against information loss");
  *   - the first-frame key enhancement of Eq. (1) (Sec. 3.4), applied on the
- *     fly by the calls that take a key_scale.
+ *     fly by the calls that take a key_scale;
+ *   - what a layer does to the projected Q and K before any of these: norm and
+ *     rotation by position (chorus_qk_norm_rope);
+ *   - attention over packed sequences of different lengths, causal or not, with
+ *     grouped heads, key caches and a prefix that all sequences share
+ *     (chorus_plan_packed_attn, chorus_packed_attn_fwd).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -484,6 +489,121 @@ size_t chorus_visit_refresh_workspace_size(const chorus_block_mask* mask);
 chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t* visited,
                                    int32_t* row_ptr, int32_t* col_idx, int64_t col_capacity,
                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Norm and rotation of Q and K, in one pass over both: what a layer does to
+ * the projected queries and keys before a mask is built from them or attention
+ * reads them.  For every token and head of x = Q and x = K:
+ *   1. norm (CHORUS_NORM_NONE: y = x): y = x / sqrt(mean(x^2) + eps) * w, the
+ *      mean over the head's 128 values with w [128] (CHORUS_NORM_HEAD) or over
+ *      the token's heads with w [heads, 128] (CHORUS_NORM_TOKEN);
+ *   2. rotation (rotary NULL: none): the head's 64 pairs of values are dealt
+ *      to the position axes in order, rotary->pairs[a] pairs to axis a; pair p
+ *      (values 2p and 2p + 1 if adjacent, else p and p + 64) turns by
+ *      t = position on its axis * freqs[p] radians:
+ *      (a, b) -> (a cos t - b sin t, a sin t + b cos t).
+ *      A pair with freqs[p] = 0 does not turn.
+ * Everything in fp32 (the angle in float64), rounded once to the type of x.
+ * Sums of squares are fp32: values above 2^60 overflow them.
+ *
+ * q, k          : [B, S, heads, 128] f16 or bf16 (dtype); shape->H heads for q,
+ *                 kv_heads for k.  k = NULL (then k_out NULL, kv_heads 0) does
+ *                 q alone.
+ * q_weight, k_weight : device float32, contiguous, 16-byte aligned; NULL
+ *                 exactly for CHORUS_NORM_NONE (and k_weight without k).
+ * eps           : >= 0 and finite.
+ * rotary        : host struct, read before the call returns.
+ * positions     : device int32, the token's position on axis a in request b at
+ *                 positions[a * pos_stride_axis + b * pos_stride_b + s]
+ *                 (strides >= 0; pos_stride_b = 0 shares them); any value.
+ * q_out, k_out  : as q and k; the same tensor as the input (same pointer and
+ *                 strides) for in place, otherwise they must not overlap it.
+ * CHORUS_NORM_TOKEN supports up to 128 heads; B * S * heads < 2^31.
+ * ------------------------------------------------------------------------- */
+typedef enum { CHORUS_NORM_NONE = 0, CHORUS_NORM_HEAD = 1, CHORUS_NORM_TOKEN = 2 } chorus_norm;
+
+typedef struct {
+  int32_t n_axes;     /* 1 .. 4                                                */
+  int32_t pairs[4];   /* pairs of each axis: >= 0, 64 in sum over n_axes       */
+  int32_t adjacent;   /* 1: values (2p, 2p + 1), 0: values (p, p + 64)         */
+  double freqs[64];   /* radians per position, finite                          */
+} chorus_rotary;
+
+chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape, int32_t kv_heads,
+                                  const chorus_tensor* q, const chorus_tensor* k, chorus_norm norm,
+                                  const float* q_weight, const float* k_weight, float eps,
+                                  const chorus_rotary* rotary, const int32_t* positions,
+                                  int64_t pos_stride_axis, int64_t pos_stride_b,
+                                  const chorus_tensor* q_out, const chorus_tensor* k_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention over packed sequences: requests (or clips, prompts, single tokens)
+ * of different lengths in one launch, without padding.  Sequence i has the
+ * query rows [q_offsets[i], q_offsets[i + 1]) of q and the key rows
+ * [k_offsets[i], k_offsets[i] + m_i) of k and v, with m_i = k_lens[i], or
+ * k_offsets[i + 1] - k_offsets[i] without k_lens.  Query head h reads key head
+ * h / (q_heads / kv_heads).  Query t of n_i sees
+ *   - every row of prefix_k / prefix_v, if there is a prefix, and
+ *   - of its own keys c: all m_i, or if causal those with c <= t + m_i - n_i
+ *     (the last query sees the last key; queries ahead of the first key see
+ *     none of their own),
+ * and O, lse are those of chorus_block_sparse_attn_fwd over what it sees.  A
+ * query that sees nothing (or only logits of -inf) gives O = 0 and lse = -inf.
+ * Keys and values that no query sees may hold anything (NaN too).
+ *
+ * The work plan of a batch depends on its lengths, which live on the device:
+ * chorus_plan_packed_attn cuts every sequence's query rows into tiles and long
+ * key ranges into pieces, so that the pieces fill the GPU, and the attention
+ * call runs it, for every layer of the step alike.
+ *
+ * shape     : host struct.  max_q is a bound on the queries of one sequence (0:
+ *             unknown); it only picks tile sizes, longer sequences stay right.
+ * q_offsets : device int32 [n_seqs + 1], non-decreasing, within [0, total_q].
+ * k_offsets : device int32 [n_seqs + 1] ([n_seqs] are read with k_lens, in any
+ *             order, overlaps allowed), within [0, total_k].
+ * k_lens    : device int32 [n_seqs] or NULL.
+ * plan      : device buffer of chorus_packed_plan_bytes(shape) bytes, 256-byte
+ *             aligned.  Lengths and offsets outside these bounds are clamped
+ *             into the tensors when the plan is made, and plan[2] (int32, read
+ *             back when needed) gets the flags 1 = q_offsets, 2 = k_offsets or
+ *             k_lens.  The attention call writes nothing if the plan was made
+ *             for another shape.
+ * q, out    : [total_q, q_heads, 128], k, v: [total_k, kv_heads, 128], prefix_k,
+ *             prefix_v: [prefix, kv_heads, 128]; f16 or bf16 (dtype); stride_b
+ *             is not used.  k and v are not read if total_k = 0 (NULL allowed).
+ *             out rows of no sequence are left as they were.
+ * lse       : optional out (NULL to skip), device float32 [q_heads, total_q].
+ * workspace : device scratch of chorus_packed_attn_workspace_size(shape) bytes,
+ *             256-byte aligned.  One call at a time may use it.
+ * Results are bitwise deterministic for given lengths and inputs.  A row's
+ * rounding may depend on the other sequences of the batch (how many pieces its
+ * keys are cut into), as in chorus_block_sparse_attn_fwd.
+ * Supports q_heads a multiple of kv_heads, total_q * q_heads < 2^31 and up to
+ * 2^20 sequences.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t n_seqs;    /* >= 1                                       */
+  int32_t total_q;   /* rows of q, out; 0: nothing is done         */
+  int32_t total_k;   /* rows of k, v                               */
+  int32_t prefix;    /* rows of prefix_k, prefix_v; 0: no prefix   */
+  int32_t q_heads;
+  int32_t kv_heads;
+  int32_t D;         /* must be 128                                */
+  int32_t causal;    /* 0 or 1                                     */
+  int32_t max_q;
+} chorus_packed_shape;
+
+size_t chorus_packed_plan_bytes(const chorus_packed_shape* shape);
+chorus_status chorus_plan_packed_attn(const chorus_packed_shape* shape, const int32_t* q_offsets,
+                                      const int32_t* k_offsets, const int32_t* k_lens, void* plan,
+                                      size_t plan_bytes, void* stream);
+size_t chorus_packed_attn_workspace_size(const chorus_packed_shape* shape);
+chorus_status chorus_packed_attn_fwd(chorus_dtype dtype, const chorus_packed_shape* shape,
+                                     const chorus_tensor* q, const chorus_tensor* k, const chorus_tensor* v,
+                                     const chorus_tensor* prefix_k, const chorus_tensor* prefix_v,
+                                     float sm_scale, const void* plan, size_t plan_bytes,
+                                     const chorus_tensor* out, float* lse, void* workspace,
+                                     size_t workspace_bytes, void* stream);
 
 /* Human-readable name of a status, and the detail of the calling thread's
  * last error (empty string if none).  Both return static / thread-local

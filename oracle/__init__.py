@@ -25,6 +25,8 @@ Generation"):
   safeguard of Sec. 3.2 "Safety fallback against information loss".
 * ``guidance``   -- the first-frame key enhancement of Eq. (1) (Sec. 3.4),
   applied to K before any of the above.
+* ``rotary``     -- norm and rotation of Q and K by position.
+* ``packed``     -- attention over packed sequences of different lengths.
 
 Every function is pinned by ``tests/test_oracle_*.py`` against brute force,
 closed forms, library routines and invariants.  The one part with no outside
@@ -33,4 +35,4 @@ output or worked example for this path ("parity unpinned" against the paper
 itself; pinned against the mathematics).
 """
 
-from . import attention, fallback, fp8, guidance, mask, mass  # noqa: F401
+from . import attention, fallback, fp8, guidance, mask, mass, packed, rotary  # noqa: F401

@@ -8,6 +8,8 @@ and fails loudly if it has not been built.
 
 from .ops import (  # noqa: F401
     BlockMask,
+    PackedPlan,
+    RotaryAxes,
     VisitMap,
     attn_block_mass,
     block_sparse_attn_fwd,
@@ -18,7 +20,10 @@ from .ops import (  # noqa: F401
     build_block_mask_noalloc,
     load_library,
     mask_coverage,
+    packed_attn_fwd,
     plan_block_mask,
+    plan_packed_attn,
+    qk_norm_rope,
     quantize_fp8_blockwise,
     select_block_mask,
     validate_block_mask,

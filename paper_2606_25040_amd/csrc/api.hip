@@ -672,4 +672,216 @@ chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t
   return from_hip(launch_compact(bitmap, words, row_ptr, rows, col_idx, s), "compact");
 }
 
+// Do two [B, S, heads, 128] 16-bit tensors share memory (by the spans of their strides)?
+static bool spans_overlap(const chorus_tensor* x, int Hx, const chorus_tensor* y, int Hy, int B, int S) {
+  auto span = [&](const chorus_tensor* t, int H) {
+    return ((int64_t)(B - 1) * t->stride_b + (int64_t)(S - 1) * t->stride_s + (int64_t)(H - 1) * t->stride_h + kHeadDim) * 2;
+  };
+  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x->data), y0 = reinterpret_cast<uintptr_t>(y->data);
+  return x0 < y0 + span(y, Hy) && y0 < x0 + span(x, Hx);
+}
+
+static bool same_tensor(const chorus_tensor* x, const chorus_tensor* y) {
+  return x->data == y->data && x->stride_b == y->stride_b && x->stride_s == y->stride_s && x->stride_h == y->stride_h;
+}
+
+chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape, int32_t kv_heads,
+                                  const chorus_tensor* q, const chorus_tensor* k, chorus_norm norm,
+                                  const float* q_weight, const float* k_weight, float eps,
+                                  const chorus_rotary* rotary, const int32_t* positions, int64_t pos_stride_axis,
+                                  int64_t pos_stride_b, const chorus_tensor* q_out, const chorus_tensor* k_out,
+                                  void* stream) {
+  g_last_error[0] = 0;
+  chorus_status st;
+  if ((st = check_shape(shape))) return st;
+  if (dtype != CHORUS_F16 && dtype != CHORUS_BF16)
+    return fail(CHORUS_ERR_UNSUPPORTED, "norm and rotation take f16 or bf16 (dtype %d)", (int)dtype);
+  if ((st = check_tensor(q, "q", 2))) return st;
+  if ((st = check_tensor(q_out, "q_out", 2))) return st;
+  if (!k != !k_out || (k ? kv_heads < 1 : kv_heads != 0))
+    return fail(CHORUS_ERR_INVALID_ARG, "k, k_out and kv_heads=%d go together", kv_heads);
+  if (k && (st = check_tensor(k, "k", 2))) return st;
+  if (k && (st = check_tensor(k_out, "k_out", 2))) return st;
+  if (norm != CHORUS_NORM_NONE && norm != CHORUS_NORM_HEAD && norm != CHORUS_NORM_TOKEN)
+    return fail(CHORUS_ERR_INVALID_ARG, "norm %d unknown", (int)norm);
+  const bool normed = norm != CHORUS_NORM_NONE;
+  if (!q_weight == normed || !k_weight == (normed && k))
+    return fail(CHORUS_ERR_INVALID_ARG, "a weight is given for each tensor exactly when it is normalised");
+  if (reinterpret_cast<uintptr_t>(q_weight) % 16 || reinterpret_cast<uintptr_t>(k_weight) % 16)
+    return fail(CHORUS_ERR_INVALID_ARG, "q_weight/k_weight is not 16-byte aligned");
+  if (normed && !(std::isfinite(eps) && eps >= 0.f)) return fail(CHORUS_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (norm == CHORUS_NORM_TOKEN && (shape->H > kMaxTokenHeads || kv_heads > kMaxTokenHeads))
+    return fail(CHORUS_ERR_UNSUPPORTED, "norm over the token supports up to %d heads", kMaxTokenHeads);
+  if (!normed && !rotary) return fail(CHORUS_ERR_INVALID_ARG, "neither norm nor rotation");
+  if (!rotary != !positions) return fail(CHORUS_ERR_INVALID_ARG, "rotary and positions go together");
+  RopeArgs a = {};
+  if (rotary) {
+    if (rotary->n_axes < 1 || rotary->n_axes > 4)
+      return fail(CHORUS_ERR_INVALID_ARG, "rotary n_axes=%d outside 1 .. 4", rotary->n_axes);
+    if (rotary->adjacent != 0 && rotary->adjacent != 1)
+      return fail(CHORUS_ERR_INVALID_ARG, "rotary adjacent must be 0 or 1");
+    int64_t sum = 0;
+    for (int i = 0; i < rotary->n_axes; ++i) {
+      if (rotary->pairs[i] < 0) return fail(CHORUS_ERR_INVALID_ARG, "rotary pairs must be >= 0");
+      sum += rotary->pairs[i];
+      a.pairs[i] = rotary->pairs[i];
+    }
+    if (sum != kHeadDim / 2)
+      return fail(CHORUS_ERR_INVALID_ARG, "rotary pairs add up to %lld, not %d", (long long)sum, kHeadDim / 2);
+    for (int i = 0; i < kHeadDim / 2; ++i) {
+      if (!std::isfinite(rotary->freqs[i])) return fail(CHORUS_ERR_INVALID_ARG, "rotary freqs must be finite");
+      a.freqs[i] = rotary->freqs[i];
+    }
+    if (pos_stride_axis < 0 || pos_stride_b < 0) return fail(CHORUS_ERR_INVALID_ARG, "positions have a negative stride");
+    if (reinterpret_cast<uintptr_t>(positions) % 4) return fail(CHORUS_ERR_INVALID_ARG, "positions are not aligned");
+    a.n_axes = rotary->n_axes;
+    a.adjacent = rotary->adjacent;
+  }
+  const int64_t heads = std::max(shape->H, kv_heads);
+  if ((int64_t)shape->B * shape->S > INT32_MAX / heads)
+    return fail(CHORUS_ERR_UNSUPPORTED, "B * S * heads exceeds 2^31");
+  if ((!same_tensor(q, q_out) && spans_overlap(q, shape->H, q_out, shape->H, shape->B, shape->S)) ||
+      (k && ((!same_tensor(k, k_out) && spans_overlap(k, kv_heads, k_out, kv_heads, shape->B, shape->S)))))
+    return fail(CHORUS_ERR_INVALID_ARG, "an output overlaps its input without being the same tensor");
+  a.q = targ(q);
+  a.q_out = targ(q_out);
+  if (k) {
+    a.k = targ(k);
+    a.k_out = targ(k_out);
+  }
+  a.q_weight = q_weight;
+  a.k_weight = k_weight;
+  a.positions = positions;
+  a.pos_axis = pos_stride_axis;
+  a.pos_b = pos_stride_b;
+  a.B = shape->B;
+  a.S = shape->S;
+  a.Hq = shape->H;
+  a.Hk = kv_heads;
+  a.norm = norm;
+  a.eps = eps;
+  return from_hip(launch_qk_norm_rope(dtype, a, static_cast<hipStream_t>(stream)), "qk_norm_rope");
+}
+
+static chorus_status check_packed_shape(const chorus_packed_shape* s) {
+  if (!s) return fail(CHORUS_ERR_INVALID_ARG, "shape is NULL");
+  if (s->n_seqs < 1 || s->total_q < 0 || s->total_k < 0 || s->prefix < 0 || s->max_q < 0)
+    return fail(CHORUS_ERR_INVALID_ARG, "packed shape n_seqs=%d must be >= 1; total_q=%d, total_k=%d, prefix=%d, max_q=%d >= 0",
+                s->n_seqs, s->total_q, s->total_k, s->prefix, s->max_q);
+  if (s->q_heads < 1 || s->kv_heads < 1 || s->q_heads % s->kv_heads)
+    return fail(CHORUS_ERR_INVALID_ARG, "q_heads=%d must be a multiple of kv_heads=%d >= 1", s->q_heads, s->kv_heads);
+  if (s->D != kHeadDim) return fail(CHORUS_ERR_UNSUPPORTED, "head dim D=%d unsupported (only 128)", s->D);
+  if (s->causal != 0 && s->causal != 1) return fail(CHORUS_ERR_INVALID_ARG, "causal must be 0 or 1");
+  if (s->n_seqs > (1 << 20)) return fail(CHORUS_ERR_UNSUPPORTED, "more than 2^20 sequences");
+  if ((int64_t)s->total_q * s->q_heads > INT32_MAX || s->kv_heads > 65535 ||
+      (int64_t)packed_config(*s).max_items * s->kv_heads > INT32_MAX / 2)
+    return fail(CHORUS_ERR_UNSUPPORTED, "too many query rows");
+  return CHORUS_OK;
+}
+
+size_t chorus_packed_plan_bytes(const chorus_packed_shape* shape) {
+  if (check_packed_shape(shape) != CHORUS_OK) return 0;
+  size_t bytes = 0;
+  carve_packed_plan(nullptr, shape->n_seqs, packed_config(*shape), &bytes);
+  return bytes;
+}
+
+static chorus_status check_plan(const void* plan, size_t have, size_t need) {
+  if (!plan) return fail(CHORUS_ERR_INVALID_ARG, "plan is NULL");
+  if (reinterpret_cast<uintptr_t>(plan) % 256) return fail(CHORUS_ERR_INVALID_ARG, "plan is not 256-byte aligned");
+  if (have < need) return fail(CHORUS_ERR_CAPACITY, "plan %zu bytes < required %zu", have, need);
+  return CHORUS_OK;
+}
+
+chorus_status chorus_plan_packed_attn(const chorus_packed_shape* shape, const int32_t* q_offsets,
+                                      const int32_t* k_offsets, const int32_t* k_lens, void* plan, size_t plan_bytes,
+                                      void* stream) {
+  g_last_error[0] = 0;
+  chorus_status st;
+  if ((st = check_packed_shape(shape))) return st;
+  if (!q_offsets || !k_offsets) return fail(CHORUS_ERR_INVALID_ARG, "q_offsets/k_offsets is NULL");
+  for (const int32_t* p : {q_offsets, k_offsets, k_lens})
+    if (reinterpret_cast<uintptr_t>(p) % 4) return fail(CHORUS_ERR_INVALID_ARG, "offsets or lengths are not aligned");
+  const PackedConfig c = packed_config(*shape);
+  size_t need = 0;
+  const PackedPlan p = carve_packed_plan(plan, shape->n_seqs, c, &need);
+  if ((st = check_plan(plan, plan_bytes, need))) return st;
+  return from_hip(launch_packed_plan(*shape, c, q_offsets, k_offsets, k_lens, p, static_cast<hipStream_t>(stream)),
+                  "packed_plan");
+}
+
+// Unfinished results: per slot, key head and row of a tile 128 values of O, the running maximum and the sum.
+static void carve_parts(void* ws, const chorus_packed_shape& s, const PackedConfig& c, float** o, float** ml, size_t* bytes) {
+  Carver v(ws);
+  const size_t rows = (size_t)c.max_slots * s.kv_heads * 32 * c.waves;
+  *o = v.take<float>(rows * kHeadDim);
+  *ml = v.take<float>(rows * 2);
+  *bytes = align_up(v.used, 256);
+}
+
+size_t chorus_packed_attn_workspace_size(const chorus_packed_shape* shape) {
+  if (check_packed_shape(shape) != CHORUS_OK) return 0;
+  float *o, *ml;
+  size_t bytes = 0;
+  carve_parts(nullptr, *shape, packed_config(*shape), &o, &ml, &bytes);
+  return bytes;
+}
+
+chorus_status chorus_packed_attn_fwd(chorus_dtype dtype, const chorus_packed_shape* shape, const chorus_tensor* q,
+                                     const chorus_tensor* k, const chorus_tensor* v, const chorus_tensor* prefix_k,
+                                     const chorus_tensor* prefix_v, float sm_scale, const void* plan, size_t plan_bytes,
+                                     const chorus_tensor* out, float* lse, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  g_last_error[0] = 0;
+  chorus_status st;
+  if ((st = check_packed_shape(shape))) return st;
+  if (dtype != CHORUS_F16 && dtype != CHORUS_BF16)
+    return fail(CHORUS_ERR_UNSUPPORTED, "packed attention takes f16 or bf16 (dtype %d)", (int)dtype);
+  if (shape->total_q == 0) return CHORUS_OK;
+  const chorus_tensor none = {nullptr, 0, 0, 0};
+  struct {
+    const chorus_tensor* t;
+    const char* name;
+    bool needed;
+  } all[] = {{q, "q", true},
+             {out, "out", true},
+             {k, "k", shape->total_k > 0},
+             {v, "v", shape->total_k > 0},
+             {prefix_k, "prefix_k", shape->prefix > 0},
+             {prefix_v, "prefix_v", shape->prefix > 0}};
+  for (const auto& x : all) {
+    if (x.needed && (st = check_tensor(x.t, x.name, 2))) return st;
+    // a key block's rows are addressed with 32-bit byte offsets from its first
+    if (x.needed && x.t->stride_s > INT32_MAX / (2 * kBlock))
+      return fail(CHORUS_ERR_UNSUPPORTED, "%s token stride too large for 32-bit offsets in a block", x.name);
+  }
+  if (shape->prefix == 0 && (prefix_k || prefix_v)) return fail(CHORUS_ERR_INVALID_ARG, "prefix tensors without a prefix");
+  if (!std::isfinite(sm_scale) || !(sm_scale > 0.f))
+    return fail(CHORUS_ERR_INVALID_ARG, "sm_scale must be finite and > 0");
+  const PackedConfig c = packed_config(*shape);
+  PackedArgs a;
+  size_t need = 0;
+  a.plan = carve_packed_plan(const_cast<void*>(plan), shape->n_seqs, c, &need);
+  if ((st = check_plan(plan, plan_bytes, need))) return st;
+  carve_parts(workspace, *shape, c, &a.part_o, &a.part_ml, &need);
+  if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+  a.q = targ(q);
+  a.o = targ(out);
+  a.k = targ(shape->total_k > 0 ? k : &none);
+  a.v = targ(shape->total_k > 0 ? v : &none);
+  a.pk = targ(shape->prefix > 0 ? prefix_k : &none);
+  a.pv = targ(shape->prefix > 0 ? prefix_v : &none);
+  a.lse = lse;
+  a.total_q = shape->total_q;
+  a.prefix = shape->prefix;
+  a.Hk = shape->kv_heads;
+  a.group = shape->q_heads / shape->kv_heads;
+  a.causal = shape->causal;
+  a.pooled = c.pooled;
+  a.max_items = c.max_items;
+  a.key = c.key;
+  a.sm_scale = sm_scale;
+  return from_hip(launch_packed_attn(dtype, c, a, static_cast<hipStream_t>(stream)), "packed_attn");
+}
+
 }  // extern "C"

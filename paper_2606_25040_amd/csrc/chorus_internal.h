@@ -14,6 +14,7 @@ constexpr int kBlock = 64;            // tokens per mask block
 constexpr int kHeadDim = 128;         // supported head dim
 constexpr int kMaxBuilderBlocks = 4096;
 constexpr int kNumXcd = 8;            // MI355X: 8 XCDs x 32 CUs
+constexpr int kMaxTokenHeads = 128;   // of a norm over the whole token
 
 // Record a formatted error for chorus_last_error(); returns `st` for chaining.
 chorus_status fail(chorus_status st, const char* fmt, ...);
@@ -124,5 +125,76 @@ struct AttnArgs {
 };
 hipError_t launch_attn_fwd_16(chorus_dtype dt, const AttnArgs& a, hipStream_t st);
 hipError_t launch_attn_fwd_fp8(const AttnArgs& a, hipStream_t st);
+
+// ---- norm and rotation of Q and K (qk_norm_rope.hip) ----
+struct RopeArgs {
+  TensorArg q, k, q_out, k_out;
+  const float* q_weight;
+  const float* k_weight;
+  const int32_t* positions;
+  int64_t pos_axis, pos_b;
+  int B, S, Hq, Hk;        // Hk == 0: q alone
+  chorus_norm norm;
+  float eps;
+  int n_axes;              // 0: no rotation
+  int pairs[4];
+  int adjacent;
+  double freqs[kHeadDim / 2];
+};
+hipError_t launch_qk_norm_rope(chorus_dtype dt, const RopeArgs& a, hipStream_t st);
+
+// ---- attention over packed sequences (packed_plan.hip, packed_attn.hip) ----
+// How a shape is cut, from host-known sizes only; the same for the plan and
+// the attention that runs it.
+struct PackedConfig {
+  int waves;           // of 32 query rows: a tile has 32 * waves rows
+  int pooled;          // the prefix is a pass of its own over the rows of all sequences
+  int per_head;        // pieces of one key head that fill the GPU
+  int32_t max_items, max_slots, max_joins;   // what a plan can come to
+  int32_t key;         // of the shape, in the plan's header
+};
+PackedConfig packed_config(const chorus_packed_shape& s);
+
+// Plan buffer (int32): header, one PackedSeq per sequence and one behind, items, joins.
+constexpr int kPlanItems = 0, kPlanJoins = 1, kPlanFlags = 2, kPlanKey = 3, kPlanPrefixPieces = 4, kPlanFirstRow = 5;
+constexpr int kPlanHeader = 16;
+struct PackedSeq {     // rows of q from q0 (to the next one's), first tile, key rows
+  int32_t q0, tile0, k0, nk;
+};
+// One workgroup's work for one key head: the query rows [row0, row0 + tile) of
+// the sequence that starts at query q0 and has `rows` of them (row = query *
+// group + head in group), over its key blocks [j0, j1).  k0 = -1: rows of all
+// sequences against the prefix.  slot: where the unfinished result goes, -1:
+// it is finished and goes to out.
+struct PackedItem {
+  int32_t q0, row0, rows, j0, j1, k0, nk, slot;
+};
+// Rows [row0, row0 + tile) of a sequence whose result is in the slots slot ..
+// slot + pieces - 1, and in the prefix' slots.
+struct PackedJoin {
+  int32_t q0, row0, rows, slot, pieces, unused[3];
+};
+struct PackedPlan {
+  int32_t* header;
+  PackedSeq* seqs;
+  PackedItem* items;
+  PackedJoin* joins;
+};
+PackedPlan carve_packed_plan(void* plan, int n_seqs, const PackedConfig& c, size_t* bytes);
+
+struct PackedArgs {
+  TensorArg q, k, v, pk, pv, o;
+  PackedPlan plan;
+  float* lse;              // nullable
+  float* part_o;           // [slot][key head][row][128]
+  float* part_ml;          // [slot][key head][row][2]: running maximum (log2), sum
+  int total_q, prefix, Hk, group, causal, pooled;
+  int max_items;
+  int32_t key;
+  float sm_scale;
+};
+hipError_t launch_packed_plan(const chorus_packed_shape& s, const PackedConfig& c, const int32_t* q_offsets,
+                              const int32_t* k_offsets, const int32_t* k_lens, const PackedPlan& plan, hipStream_t st);
+hipError_t launch_packed_attn(chorus_dtype dt, const PackedConfig& c, const PackedArgs& a, hipStream_t st);
 
 }  // namespace chorus

@@ -1,0 +1,255 @@
+// Work plan of attention over packed sequences: from the lengths on the device to a list of workgroups.
+//
+// Every sequence's query rows (query * group + head in group, so that the heads that share a key head share its
+// tiles) are cut into tiles of 32 * waves rows, and a tile's key blocks (64 keys) into pieces where whole tiles
+// would leave the GPU unevenly filled: with C key blocks in all, a piece has about C / per_head blocks.  A prefix
+// is either part of each tile's key blocks, or, pooled, a pass of its own whose tiles run over the rows of all
+// sequences, so its keys are read once per tile of rows and not once per sequence.  Items are listed longest
+// first (by 64 classes of length), so the last workgroups to start are the shortest.
+//
+// One workgroup: three passes over the tiles (cost, classes, emission) with two block scans, a few microseconds.
+// A plan never exceeds packed_config's bounds: the extra pieces of a cut come to at most C / chunk <= per_head.
+#include <algorithm>
+
+#include "chorus_internal.h"
+
+namespace chorus {
+
+// chunk: blocks per piece at least, so that a piece is worth its launch and its share of the join.
+constexpr int kMinChunk = 4;
+constexpr int kClasses = 64;
+
+PackedPlan carve_packed_plan(void* plan, int n_seqs, const PackedConfig& c, size_t* bytes) {
+  Carver v(plan);
+  PackedPlan p;
+  p.header = v.take<int32_t>(kPlanHeader);
+  p.seqs = v.take<PackedSeq>((size_t)n_seqs + 1);
+  p.items = v.take<PackedItem>(c.max_items);
+  p.joins = v.take<PackedJoin>(c.max_joins);
+  if (bytes) *bytes = align_up(v.used, 256);
+  return p;
+}
+
+PackedConfig packed_config(const chorus_packed_shape& s) {
+  PackedConfig c;
+  const int group = s.q_heads / s.kv_heads;
+  const int64_t rows = (int64_t)s.total_q * group;
+  c.waves = 4;
+  const int tile = 32 * c.waves;
+  // The prefix is worth a pass of its own when the sequences' own tiles are mostly empty: then a tile of pooled
+  // rows replaces several walks over it.
+  c.pooled = s.prefix > 0 && s.n_seqs > 1 && rows < (int64_t)s.n_seqs * tile;
+  c.per_head = (512 + s.kv_heads - 1) / s.kv_heads;
+  const int64_t tiles = rows / tile + s.n_seqs, pooled_tiles = c.pooled ? rows / tile + 1 : 0;
+  c.max_items = (int32_t)(tiles + pooled_tiles + c.per_head);
+  c.max_slots = c.pooled ? c.max_items : 2 * c.per_head;
+  c.max_joins = c.pooled ? (int32_t)tiles : c.per_head;
+  uint32_t h = 2166136261u;
+  for (const int32_t v : {s.n_seqs, s.total_q, s.total_k, s.prefix, s.q_heads, s.kv_heads, s.causal, s.max_q})
+    h = (h ^ (uint32_t)v) * 16777619u + 0x9e3779b9u;
+  c.key = (int32_t)h;
+  return c;
+}
+
+namespace {
+
+constexpr int kThreads = 1024;
+
+struct PlanArgs {
+  const int32_t* q_offsets;
+  const int32_t* k_offsets;
+  const int32_t* k_lens;
+  PackedPlan plan;
+  int n_seqs, total_q, total_k, prefix, group, causal, tile, pooled, per_head;
+  int32_t key;
+};
+
+// Inclusive scan over the workgroup (every thread takes part); `total` is the last thread's value.
+template <class Op>
+__device__ inline int block_scan(int v, Op op, int* wave_s, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int u = __shfl_up(v, d);
+    if (lane >= d) v = op(u, v);
+  }
+  __syncthreads();
+  if (lane == 63) wave_s[wave] = v;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w == wave && w > 0) v = op(before, v);
+    before = w ? op(before, wave_s[w]) : wave_s[0];
+  }
+  *total = before;
+  return v;
+}
+
+struct Add {
+  __device__ int operator()(int a, int b) const { return a + b; }
+};
+struct Max {
+  __device__ int operator()(int a, int b) const { return a > b ? a : b; }
+};
+
+struct Tile {
+  PackedSeq seq;
+  int row0, rows, blocks;
+};
+
+__device__ inline Tile tile_at(const PlanArgs& a, int t) {
+  int lo = 0, hi = a.n_seqs;   // the last sequence whose first tile is at or before t
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.plan.seqs[mid].tile0 <= t)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  Tile x;
+  x.seq = a.plan.seqs[lo];
+  const int nq = a.plan.seqs[lo + 1].q0 - x.seq.q0;
+  x.rows = nq * a.group;
+  x.row0 = (t - x.seq.tile0) * a.tile;
+  int seen = x.seq.nk;
+  if (a.causal) {
+    const int last = (min(x.row0 + a.tile, x.rows) - 1) / a.group;
+    seen = min(max(last + 1 + seen - nq, 0), seen);
+  }
+  x.blocks = (seen + kBlock - 1) / kBlock + (a.pooled ? 0 : (a.prefix + kBlock - 1) / kBlock);
+  return x;
+}
+
+__global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
+  __shared__ int wave_s[kThreads / 64];
+  __shared__ unsigned long long cost_s;
+  __shared__ int flags_s, class_s[kClasses];
+  const int tid = threadIdx.x, N = a.n_seqs;
+  if (tid == 0) {
+    cost_s = 0;
+    flags_s = 0;
+  }
+  if (tid < kClasses) class_s[tid] = 0;
+  __syncthreads();
+
+  int run = 0, total;
+  for (int base = 0; base <= N; base += kThreads) {
+    const int i = base + tid;
+    const int raw = i <= N ? a.q_offsets[i] : 0;
+    const int v = max(run, block_scan(min(max(raw, 0), a.total_q), Max(), wave_s, &total));
+    run = max(run, total);
+    if (i <= N) {
+      a.plan.seqs[i].q0 = v;
+      if (v != raw) atomicOr(&flags_s, 1);
+    }
+  }
+  __syncthreads();
+  run = 0;
+  for (int base = 0; base < N; base += kThreads) {
+    const int i = base + tid;
+    int tiles = 0;
+    if (i < N) {
+      const int64_t rows = (int64_t)(a.plan.seqs[i + 1].q0 - a.plan.seqs[i].q0) * a.group;
+      tiles = (int)((rows + a.tile - 1) / a.tile);
+    }
+    const int upto = run + block_scan(tiles, Add(), wave_s, &total);
+    run += total;
+    if (i < N) {
+      const int raw0 = a.k_offsets[i];
+      const int64_t raw = a.k_lens ? a.k_lens[i] : (int64_t)a.k_offsets[i + 1] - raw0;
+      const int k0 = min(max(raw0, 0), a.total_k);
+      const int nk = (int)min(max(raw, (int64_t)0), (int64_t)(a.total_k - k0));
+      if (k0 != raw0 || nk != raw) atomicOr(&flags_s, 2);
+      a.plan.seqs[i].tile0 = upto - tiles;
+      a.plan.seqs[i].k0 = k0;
+      a.plan.seqs[i].nk = nk;
+    }
+  }
+  const int n_tiles = run;
+  __syncthreads();
+
+  const int first = a.plan.seqs[0].q0;
+  const int pooled_rows = (a.plan.seqs[N].q0 - first) * a.group;
+  const int pooled_tiles = a.pooled ? (pooled_rows + a.tile - 1) / a.tile : 0;
+  const int prefix_blocks = (a.prefix + kBlock - 1) / kBlock;
+  unsigned long long cost = 0;
+  for (int t = tid; t < n_tiles; t += kThreads) cost += tile_at(a, t).blocks;
+  if (cost) atomicAdd(&cost_s, cost);
+  __syncthreads();
+  cost = cost_s + (unsigned long long)pooled_tiles * prefix_blocks;
+  const int chunk = (int)min((cost + a.per_head - 1) / a.per_head + 0ull, (unsigned long long)(1 << 26));
+  const int piece = max(chunk, kMinChunk), longest = piece + piece / 2;
+  auto pieces = [&](int blocks) { return blocks > longest ? (blocks + piece - 1) / piece : 1; };
+  auto class_of = [&](int blocks, int p) {
+    return kClasses - 1 - (int)((int64_t)((blocks + p - 1) / p) * kClasses / (longest + 1));
+  };
+  const int np = pooled_tiles ? pieces(prefix_blocks) : 0;
+
+  for (int t = tid; t < n_tiles; t += kThreads) {
+    const int n = tile_at(a, t).blocks, p = pieces(n);
+    if (n > 0 || !a.pooled) atomicAdd(&class_s[class_of(n, p)], p);
+  }
+  if (tid == 0 && np) atomicAdd(&class_s[class_of(prefix_blocks, np)], pooled_tiles * np);
+  __syncthreads();
+  if (tid < kClasses) {   // first position of each class
+    int v = class_s[tid];
+    const int own = v;
+#pragma unroll
+    for (int d = 1; d < kClasses; d *= 2) {
+      const int u = __shfl_up(v, d);
+      if (tid >= d) v += u;
+    }
+    class_s[tid] = v - own;
+    if (tid == kClasses - 1) a.plan.header[kPlanItems] = v;
+  }
+  __syncthreads();
+
+  for (int x = tid; x < pooled_tiles * np; x += kThreads) {
+    const int t = x / np, i = x % np;
+    const int at = atomicAdd(&class_s[class_of(prefix_blocks, np)], 1);
+    a.plan.items[at] = {first, t * a.tile, pooled_rows, (int)((int64_t)i * prefix_blocks / np),
+                        (int)((int64_t)(i + 1) * prefix_blocks / np), -1, 0, x};
+  }
+  int slots = pooled_tiles * np, joins = 0;
+  for (int base = 0; base < n_tiles; base += kThreads) {
+    const int t = base + tid;
+    Tile x = {};
+    int p = 0, own = 0, joined = 0;
+    if (t < n_tiles) {
+      x = tile_at(a, t);
+      p = a.pooled && x.blocks == 0 ? 0 : pieces(x.blocks);
+      joined = a.pooled || p > 1;
+      own = joined ? p : 0;
+    }
+    int slot_total, join_total;
+    const int slot = slots + block_scan(own, Add(), wave_s, &slot_total) - own;
+    const int join = joins + block_scan(joined, Add(), wave_s, &join_total) - joined;
+    slots += slot_total;
+    joins += join_total;
+    for (int i = 0; i < p; ++i) {
+      const int at = atomicAdd(&class_s[class_of(x.blocks, p)], 1);
+      a.plan.items[at] = {x.seq.q0, x.row0, x.rows, (int)((int64_t)i * x.blocks / p),
+                          (int)((int64_t)(i + 1) * x.blocks / p), x.seq.k0, x.seq.nk, joined ? slot + i : -1};
+    }
+    if (joined) a.plan.joins[join] = {x.seq.q0, x.row0, x.rows, slot, p, {0, 0, 0}};
+  }
+  if (tid == 0) {
+    a.plan.header[kPlanJoins] = joins;
+    a.plan.header[kPlanFlags] = flags_s;
+    a.plan.header[kPlanKey] = a.key;
+    a.plan.header[kPlanPrefixPieces] = np;
+    a.plan.header[kPlanFirstRow] = first * a.group;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_packed_plan(const chorus_packed_shape& s, const PackedConfig& c, const int32_t* q_offsets,
+                              const int32_t* k_offsets, const int32_t* k_lens, const PackedPlan& plan, hipStream_t st) {
+  const PlanArgs a = {q_offsets, k_offsets, k_lens,   plan,       s.n_seqs, s.total_q,  s.total_k, s.prefix,
+                      s.q_heads / s.kv_heads, s.causal, 32 * c.waves, c.pooled, c.per_head, c.key};
+  hipLaunchKernelGGL(packed_plan_kernel, dim3(1), dim3(kThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace chorus

@@ -50,6 +50,16 @@ class KeyScale(ctypes.Structure):
     _fields_ = [("n_first", ctypes.c_int32), ("beta", ctypes.c_float)]
 
 
+class Rotary(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4), ("adjacent", ctypes.c_int32),
+                ("freqs", ctypes.c_double * 64)]
+
+
+class PackedShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "total_q", "total_k", "prefix", "q_heads", "kv_heads", "D",
+                                              "causal", "max_q")]
+
+
 def _key_scale(key_scale):
     """(n_first, beta) -> pointer to a chorus_key_scale, None -> NULL."""
     if key_scale is None:
@@ -69,6 +79,8 @@ EXPORTS = [
     "chorus_mask_coverage",
     "chorus_visit_map_bytes", "chorus_visit_reset", "chorus_visit_update",
     "chorus_visit_refresh_workspace_size", "chorus_visit_refresh",
+    "chorus_qk_norm_rope", "chorus_packed_plan_bytes", "chorus_plan_packed_attn",
+    "chorus_packed_attn_workspace_size", "chorus_packed_attn_fwd",
     "chorus_status_string", "chorus_last_error", "chorus_version",
 ]
 
@@ -125,6 +137,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "chorus_visit_update": (I32, [P(Mask), VP, VP]),
         "chorus_visit_refresh_workspace_size": (SZ, [P(Mask)]),
         "chorus_visit_refresh": (I32, [P(Mask), VP, VP, VP, I64, VP, SZ, VP]),
+        "chorus_qk_norm_rope": (I32, [I32, P(Shape), I32, P(Tensor), P(Tensor), I32, VP, VP, F32, P(Rotary), VP, I64,
+                                      I64, P(Tensor), P(Tensor), VP]),
+        "chorus_packed_plan_bytes": (SZ, [P(PackedShape)]),
+        "chorus_plan_packed_attn": (I32, [P(PackedShape), VP, VP, VP, VP, SZ, VP]),
+        "chorus_packed_attn_workspace_size": (SZ, [P(PackedShape)]),
+        "chorus_packed_attn_fwd": (I32, [I32, P(PackedShape), P(Tensor), P(Tensor), P(Tensor), P(Tensor), P(Tensor),
+                                         F32, VP, SZ, P(Tensor), VP, VP, SZ, VP]),
         "chorus_status_string": (ctypes.c_char_p, [I32]),
         "chorus_last_error": (ctypes.c_char_p, []),
         "chorus_version": (I32, []),
@@ -593,3 +612,186 @@ class VisitMap:
         w = self.bits.cpu().numpy().view(np.uint32).reshape(-1, self.words)
         bits = ((w[:, :, None] >> np.arange(32, dtype=np.uint32)) & 1).astype(bool)
         return bits.reshape(w.shape[0], -1)[:, : self.n_kv]
+
+
+def _current(*tensors) -> None:
+    """Every given tensor lives on the current device, whose stream the call is put on."""
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("expected a device tensor")
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _writable(t: torch.Tensor, name: str) -> None:
+    """Rows of an output do not share memory: each stride reaches past what the smaller ones span."""
+    reach = 1
+    for size, stride in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n > 1), key=lambda x: x[1]):
+        if stride < reach:
+            raise ValueError(f"{name} has rows that share memory")
+        reach = stride * (size - 1) + reach
+
+
+class RotaryAxes:
+    """A rotation of 64 pairs per head dealt to position axes: ``pairs[a]`` pairs to axis a, in order; pair p turns
+    by position * ``freqs[p]`` radians.  ``freqs=None``: each axis has the ladder theta^(-i / pairs[a]), i = 0 ..
+    pairs[a] - 1.  ``adjacent`` pairs are the values (2p, 2p + 1) of a head, others (p, p + 64)."""
+
+    def __init__(self, pairs, freqs=None, adjacent: bool = True, theta: float = 10000.0):
+        pairs = [int(n) for n in pairs]
+        if not 1 <= len(pairs) <= 4 or any(n < 0 for n in pairs) or sum(pairs) != 64:
+            raise ValueError("pairs must hold 1 to 4 counts >= 0 that add up to 64")
+        if freqs is None:
+            freqs = [float(theta) ** (-i / n) for n in pairs for i in range(n)]
+        freqs = [float(f) for f in freqs]
+        if len(freqs) != 64 or not all(math.isfinite(f) for f in freqs):
+            raise ValueError("freqs must hold 64 finite values")
+        self.pairs, self.freqs, self.adjacent = tuple(pairs), tuple(freqs), bool(adjacent)
+        self.c = Rotary(len(pairs), (ctypes.c_int32 * 4)(*pairs), int(self.adjacent), (ctypes.c_double * 64)(*freqs))
+
+
+_NORMS = {None: 0, "head": 1, "token": 2}
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None = None, rotary: RotaryAxes | None = None,
+                 positions: torch.Tensor | None = None, norm: str | None = None, q_weight: torch.Tensor | None = None,
+                 k_weight: torch.Tensor | None = None, eps: float = 1e-6, q_out: torch.Tensor | None = None,
+                 k_out: torch.Tensor | None = None):
+    """chorus_qk_norm_rope: norm and rotation of ``q [B, S, H, 128]`` and ``k [B, S, Hk, 128]`` (f16 or bf16) in one
+    pass; returns (q_out, k_out), or q_out alone without ``k``.
+
+    ``norm``: "head" (fp32 weights [128]), "token" (over a token's heads, weights [heads, 128]) or None.
+    ``positions``: int32 [axes, S] (shared by the requests) or [axes, B, S].  ``q_out`` / ``k_out`` may be the
+    inputs themselves."""
+    L = load_library()
+    if norm not in _NORMS:
+        raise ValueError("norm must be None, 'head' or 'token'")
+    _current(q, k, positions, q_weight, k_weight, q_out, k_out)
+    dt = _dtype_code(q)
+    if q.dim() != 4:
+        raise ValueError("expected a [B, S, H, D] tensor")
+    B, S, H, D = q.shape
+    Hk = 0
+    if k is not None:
+        if k.dim() != 4 or k.dtype != q.dtype or (k.shape[0], k.shape[1], k.shape[3]) != (B, S, D):
+            raise ValueError("k must share q's dtype, requests, tokens and head dim")
+        Hk = k.shape[2]
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    for w, heads in ((q_weight, H), (k_weight, Hk)):
+        if w is None:
+            continue
+        shapes = ((D,),) if norm == "head" else ((heads, D), (heads * D,))
+        if norm is None or w.dtype != torch.float32 or tuple(w.shape) not in shapes or not w.is_contiguous():
+            raise ValueError("a weight must be a contiguous float32 tensor, [128] for norm='head', [heads, 128] for 'token'")
+    if (rotary is None) != (positions is None):
+        raise ValueError("rotary and positions go together")
+    axis_stride = batch_stride = 0
+    if rotary is not None:
+        if positions.dtype != torch.int32 or positions.dim() not in (2, 3) or positions.shape[0] != len(rotary.pairs) \
+                or positions.shape[-1] != S or (positions.dim() == 3 and positions.shape[1] != B) \
+                or (positions.stride(-1) != 1 and S > 1):
+            raise ValueError("positions must be int32 [axes, S] or [axes, B, S] with contiguous tokens")
+        axis_stride = positions.stride(0)
+        batch_stride = positions.stride(1) if positions.dim() == 3 else 0
+    if q_out is None:
+        q_out = torch.empty((B, S, H, D), dtype=q.dtype, device=q.device)
+    elif q_out.shape != q.shape or q_out.dtype != q.dtype:
+        raise ValueError("q_out must have q's shape and dtype")
+    if k is not None and k_out is None:
+        k_out = torch.empty((B, S, Hk, D), dtype=k.dtype, device=k.device)
+    elif k is not None and (k_out.shape != k.shape or k_out.dtype != k.dtype):
+        raise ValueError("k_out must have k's shape and dtype")
+    _writable(q_out, "q_out")
+    if k is not None:
+        _writable(k_out, "k_out")
+    st = L.chorus_qk_norm_rope(dt, ctypes.byref(_shape(q)), Hk, ctypes.byref(_tensor(q)),
+                               None if k is None else ctypes.byref(_tensor(k)), _NORMS[norm], _ptr(q_weight),
+                               _ptr(k_weight), float(eps), None if rotary is None else ctypes.byref(rotary.c),
+                               _ptr(positions), axis_stride, batch_stride, ctypes.byref(_tensor(q_out)),
+                               None if k is None else ctypes.byref(_tensor(k_out)), _stream())
+    _check(st, "chorus_qk_norm_rope")
+    return q_out if k is None else (q_out, k_out)
+
+
+@dataclass
+class PackedPlan:
+    """Work plan of a batch of packed sequences (chorus_plan_packed_attn), for every layer of a step."""
+    data: torch.Tensor       # uint8; the plan starts at its first 256-byte boundary
+    shape: PackedShape
+
+    def flags(self) -> int:
+        """Synchronises; 0, or 1 (q_offsets) | 2 (k_offsets, k_lens) where offsets or lengths had to be clamped."""
+        at = _aligned(self.data) - self.data.data_ptr()
+        return int(self.data[at:at + 64].view(torch.int32)[2].item())
+
+
+def plan_packed_attn(q_offsets: torch.Tensor, k_offsets: torch.Tensor, total_q: int, total_k: int, q_heads: int,
+                     kv_heads: int, causal: bool = True, k_lens: torch.Tensor | None = None, prefix: int = 0,
+                     max_q: int = 0, out: PackedPlan | None = None) -> PackedPlan:
+    """chorus_plan_packed_attn: the plan for N sequences with query rows ``q_offsets[i] : q_offsets[i + 1]`` of
+    ``total_q`` and key rows from ``k_offsets[i]`` of ``total_k``, ``k_lens[i]`` of them (without ``k_lens`` up to
+    ``k_offsets[i + 1]``).  ``q_offsets``: int32 [N + 1] on the device; ``k_offsets`` likewise, or [N] with
+    ``k_lens`` [N].  ``prefix``: rows of a prefix that every sequence sees.  ``max_q``: the longest sequence's
+    queries, if known.  ``out``: a plan of the same shape to write again."""
+    L = load_library()
+    _current(q_offsets, k_offsets, k_lens)
+    N = q_offsets.numel() - 1
+    for t, name in ((q_offsets, "q_offsets"), (k_offsets, "k_offsets"), (k_lens, "k_lens")):
+        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous int32 vector")
+    if N < 1 or k_offsets.numel() < (N if k_lens is not None else N + 1) or (k_lens is not None and k_lens.numel() != N):
+        raise ValueError("q_offsets holds N + 1 entries, k_offsets N + 1 (N with k_lens), k_lens N")
+    shape = PackedShape(N, int(total_q), int(total_k), int(prefix), int(q_heads), int(kv_heads), 128, int(bool(causal)),
+                        int(max_q))
+    need = L.chorus_packed_plan_bytes(ctypes.byref(shape))
+    if out is None:
+        out = PackedPlan(torch.empty(need + 256, dtype=torch.uint8, device=q_offsets.device), shape)
+    elif bytes(out.shape) != bytes(shape):
+        raise ValueError("out is a plan of another shape")
+    _current(out.data)
+    st = L.chorus_plan_packed_attn(ctypes.byref(shape), q_offsets.data_ptr(), k_offsets.data_ptr(), _ptr(k_lens),
+                                   _aligned(out.data), need, _stream())
+    _check(st, "chorus_plan_packed_attn")
+    return out
+
+
+def _rows(t: torch.Tensor, rows: int, heads: int, like: torch.Tensor, name: str) -> Tensor:
+    if t.dim() != 3 or tuple(t.shape) != (rows, heads, like.shape[-1]) or t.dtype != like.dtype:
+        raise ValueError(f"{name} must be a {like.dtype} [{rows}, {heads}, {like.shape[-1]}] tensor")
+    if t.stride(2) != 1:
+        raise ValueError("head dim must be contiguous")
+    return Tensor(t.data_ptr(), 0, t.stride(0), t.stride(1))
+
+
+def packed_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: PackedPlan, sm_scale: float | None = None,
+                    prefix_k: torch.Tensor | None = None, prefix_v: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None, return_lse: bool = False):
+    """chorus_packed_attn_fwd: attention of ``q [total_q, q_heads, 128]`` to ``k, v [total_k, kv_heads, 128]`` (and
+    ``prefix_k, prefix_v [prefix, kv_heads, 128]``) by ``plan``; f16 or bf16.  Returns ``out`` (and ``lse [q_heads,
+    total_q]`` fp32 when ``return_lse``); rows of no sequence are not written."""
+    L = load_library()
+    _current(q, k, v, prefix_k, prefix_v, out, plan.data)
+    s = plan.shape
+    dt = _dtype_code(q)
+    if (prefix_k is None) != (s.prefix == 0) or (prefix_v is None) != (s.prefix == 0):
+        raise ValueError(f"the plan's prefix has {s.prefix} rows")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ct = [_rows(q, s.total_q, s.q_heads, q, "q"), _rows(k, s.total_k, s.kv_heads, q, "k"),
+          _rows(v, s.total_k, s.kv_heads, q, "v")]
+    ct += [_rows(t, s.prefix, s.kv_heads, q, n) if s.prefix else None for t, n in ((prefix_k, "prefix_k"),
+                                                                                  (prefix_v, "prefix_v"))]
+    co = _rows(out, s.total_q, s.q_heads, q, "out")
+    _writable(out, "out")
+    lse = torch.empty((s.q_heads, s.total_q), dtype=torch.float32, device=q.device) if return_lse else None
+    sm = 1.0 / math.sqrt(q.shape[-1]) if sm_scale is None else float(sm_scale)
+    need = L.chorus_packed_attn_workspace_size(ctypes.byref(s))
+    ws = _workspace(need, q.device)
+    st = L.chorus_packed_attn_fwd(dt, ctypes.byref(s), *(None if t is None else ctypes.byref(t) for t in ct), sm,
+                                  _aligned(plan.data), plan.data.numel() - 256, ctypes.byref(co), _ptr(lse),
+                                  _aligned(ws), need, _stream())
+    _check(st, "chorus_packed_attn_fwd")
+    return (out, lse) if return_lse else out

@@ -1,0 +1,157 @@
+"""Refusals of the norm / rotation and packed attention entry points, on the host before any device call (CPU)."""
+
+import ctypes
+
+import pytest
+import torch
+
+from paper_2606_25040_amd import ops
+
+FAKE = 0x10000           # aligned, never dereferenced: every call below fails validation first
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return ops.load_library()
+
+
+def t(ss=4 * 128, sh=128, data=FAKE, sb=0):
+    return ops.Tensor(data, sb, ss, sh)
+
+
+def by(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def rotary(pairs=(22, 21, 21), adjacent=1, freq=1.0, n=None):
+    return ops.Rotary(len(pairs) if n is None else n, (ctypes.c_int32 * 4)(*pairs), adjacent, (ctypes.c_double * 64)(*[freq] * 64))
+
+
+def rope(lib, shape=(1, 10, 4, 128), Hk=4, q=None, k=..., norm=1, qw=FAKE, kw=FAKE, eps=1e-6, rot=..., pos=FAKE, pa=10, pb=0,
+         qo=None, ko=..., dtype=ops.BF16):
+    big = t(data=0x1000000)
+    k = t(data=0x2000000) if k is ... else k
+    ko = t(data=0x3000000) if ko is ... else ko
+    rot = rotary() if rot is ... else rot
+    return lib.chorus_qk_norm_rope(dtype, by(ops.Shape(*shape)), Hk, by(q or t()), by(k), norm, qw, kw, eps, by(rot), pos, pa, pb,
+                                   by(qo or big), by(ko), None)
+
+
+def test_norm_rope_refusals(lib):
+    assert rope(lib, shape=(1, 10, 4, 64)) == 2
+    assert rope(lib, shape=(0, 10, 4, 128)) == 1
+    assert rope(lib, dtype=ops.FP8_E4M3) == 2
+    assert rope(lib, k=None) == 1                                    # k_out and kv_heads without k
+    assert rope(lib, ko=None) == 1
+    assert rope(lib, Hk=0) == 1
+    assert rope(lib, norm=3) == 1
+    assert rope(lib, qw=None) == 1
+    assert rope(lib, kw=None) == 1
+    assert rope(lib, norm=0) == 1                                    # weights without a norm
+    assert rope(lib, qw=FAKE + 4) == 1
+    assert rope(lib, eps=-1.0) == 1 and rope(lib, eps=float("nan")) == 1
+    assert rope(lib, norm=2, shape=(1, 10, 129, 128)) == 2
+    assert rope(lib, norm=2, Hk=129) == 2
+    assert rope(lib, norm=0, qw=None, kw=None, rot=None, pos=None) == 1
+    assert rope(lib, rot=None) == 1 and rope(lib, pos=None) == 1
+    assert rope(lib, rot=rotary(n=0)) == 1 and rope(lib, rot=rotary(n=5)) == 1
+    assert rope(lib, rot=rotary((22, 21, 20))) == 1
+    assert rope(lib, rot=rotary((70, -6))) == 1
+    assert rope(lib, rot=rotary(adjacent=2)) == 1
+    assert rope(lib, rot=rotary(freq=float("inf"))) == 1
+    assert rope(lib, pa=-1) == 1 and rope(lib, pb=-1) == 1
+    assert rope(lib, pos=FAKE + 2) == 1
+    assert rope(lib, shape=(1 << 14, 1 << 14, 64, 128)) == 2
+    assert rope(lib, q=t(data=FAKE + 8)) == 1
+    assert rope(lib, q=t(ss=4 * 128 + 4)) == 1
+    assert rope(lib, qo=t(data=FAKE + 512)) == 1                     # overlaps its input, shifted
+    assert b"overlap" in lib.chorus_last_error()
+    assert rope(lib, qo=t(ss=8 * 128)) == 1                          # or with other strides
+
+
+def packed(n=2, tq=10, tk=20, prefix=0, H=4, Hk=2, D=128, causal=1, max_q=0):
+    return ops.PackedShape(n, tq, tk, prefix, H, Hk, D, causal, max_q)
+
+
+BAD = [(packed(n=0), 1), (packed(tq=-1), 1), (packed(tk=-1), 1), (packed(prefix=-1), 1), (packed(max_q=-1), 1), (packed(H=5), 1),
+       (packed(Hk=0), 1), (packed(H=0, Hk=1), 1), (packed(D=64), 2), (packed(causal=2), 1), (packed(n=(1 << 20) + 1), 2),
+       (packed(tq=1 << 30), 2), (packed(H=70000, Hk=70000, tq=1), 2)]
+
+
+def make_plan(lib, s, qo=FAKE, ko=FAKE, kl=None, plan=FAKE, nbytes=None):
+    need = lib.chorus_packed_plan_bytes(by(s)) if nbytes is None else nbytes
+    return lib.chorus_plan_packed_attn(by(s), qo, ko, kl, plan, need, None)
+
+
+def attend(lib, s, q=None, k=..., v=..., pk=None, pv=None, sm=0.088, plan=FAKE, nbytes=None, out=None, ws=FAKE, ws_bytes=None,
+           dtype=ops.F16):
+    need = lib.chorus_packed_plan_bytes(by(s)) if nbytes is None else nbytes
+    wsb = lib.chorus_packed_attn_workspace_size(by(s)) if ws_bytes is None else ws_bytes
+    k = t() if k is ... else k
+    v = t() if v is ... else v
+    return lib.chorus_packed_attn_fwd(dtype, by(s), by(q or t()), by(k), by(v), by(pk), by(pv), sm, plan, need, by(out or t()), None,
+                                      ws, wsb, None)
+
+
+def test_packed_shapes_are_checked_everywhere(lib):
+    for s, status in BAD:
+        assert lib.chorus_packed_plan_bytes(by(s)) == 0 and lib.chorus_packed_attn_workspace_size(by(s)) == 0
+        assert make_plan(lib, s) == status
+        assert attend(lib, s) == status
+    assert lib.chorus_packed_plan_bytes(None) == 0
+    assert lib.chorus_packed_plan_bytes(by(packed())) > 0
+
+
+def test_packed_plan_refusals(lib):
+    s = packed()
+    assert make_plan(lib, s, qo=None) == 1 and make_plan(lib, s, ko=None) == 1
+    assert make_plan(lib, s, kl=FAKE + 2) == 1
+    assert make_plan(lib, s, plan=None) == 1 and make_plan(lib, s, plan=FAKE + 16) == 1
+    assert make_plan(lib, s, nbytes=256) == 3
+
+
+def test_packed_attention_refusals(lib):
+    s = packed()
+    assert attend(lib, s, dtype=ops.FP8_E4M3) == 2
+    assert attend(lib, s, q=t(data=FAKE + 2)) == 1
+    assert attend(lib, s, k=None) == 1 and attend(lib, s, v=None) == 1
+    assert attend(lib, s, k=t(ss=1 << 30)) == 2
+    assert attend(lib, s, out=t(ss=-128)) == 1
+    assert attend(lib, s, pk=t(), pv=t()) == 1                       # a prefix that the shape does not have
+    assert attend(lib, packed(prefix=5)) == 1                        # and one that is missing
+    assert attend(lib, packed(prefix=5), pk=t()) == 1
+    assert attend(lib, s, sm=0.0) == 1 and attend(lib, s, sm=float("inf")) == 1
+    assert attend(lib, s, plan=None) == 1 and attend(lib, s, plan=FAKE + 64) == 1
+    assert attend(lib, s, nbytes=512) == 3
+    assert attend(lib, s, ws=None) == 5 and attend(lib, s, ws_bytes=256) == 5
+    assert attend(lib, packed(tq=0), q=t(data=None)) == 0            # nothing to do
+
+
+def test_python_refuses_host_tensors():
+    x = torch.zeros(1, 4, 2, 128, dtype=torch.float16)
+    with pytest.raises(ValueError, match="device tensor"):
+        ops.qk_norm_rope(x, norm="head", q_weight=torch.ones(128))
+    o = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="device tensor"):
+        ops.plan_packed_attn(o, o, 1, 1, 1, 1)
+    with pytest.raises(ValueError, match="norm must be"):
+        ops.qk_norm_rope(x, norm="batch")
+    for bad in ((64, 1), (), (10,) * 5, (65, -1)):
+        with pytest.raises(ValueError, match="pairs"):
+            ops.RotaryAxes(bad)
+    with pytest.raises(ValueError, match="freqs"):
+        ops.RotaryAxes((64,), freqs=[1.0] * 63)
+
+
+def test_ladder_of_each_axis():
+    r = ops.RotaryAxes((2, 62), theta=100.0)
+    assert r.freqs[:3] == (1.0, 100.0 ** -0.5, 1.0) and r.freqs[63] == 100.0 ** (-61 / 62)
+
+
+def test_rows_that_share_memory_are_no_output():
+    x = torch.zeros(6, 1, 128)
+    ops._writable(x, "out")
+    ops._writable(x.transpose(0, 1), "out")
+    for bad in (x[:1].expand(6, 1, 128), torch.zeros(1000).as_strided((5, 2, 128), (128, 64, 1))):
+        with pytest.raises(ValueError, match="share memory"):
+            ops._writable(bad, "out")
