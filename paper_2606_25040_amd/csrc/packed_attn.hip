@@ -11,6 +11,7 @@
 //
 // Rows cut into pieces leave (m, l, O) in fp32 in the workspace; packed_join_kernel joins them.
 #include <cfloat>
+#include <type_traits>
 
 #include "attn_common.h"
 
@@ -32,7 +33,7 @@ template <>
 struct Type<true> {
   using vec8 = bf16x8;
   using scalar = __bf16;
-  static constexpr uint32_t kExp = 0x7f807f80u, kOne = 0x3f80u, kLow = 0x00800080u;   // exponent bits, 1.0
+  static constexpr uint32_t kInf = 0x7f80u, kOne = 0x3f80u;
   static __device__ inline f32x16 mfma(vec8 a, vec8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -46,7 +47,7 @@ template <>
 struct Type<false> {
   using vec8 = f16x8;
   using scalar = _Float16;
-  static constexpr uint32_t kExp = 0x7c007c00u, kOne = 0x3c00u, kLow = 0x04000400u;
+  static constexpr uint32_t kInf = 0x7c00u, kOne = 0x3c00u;
   static __device__ inline f32x16 mfma(vec8 a, vec8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
@@ -78,13 +79,35 @@ inline int64_t packed_grid(int Hk, int max_items) {
   return kNumXcd * ((int64_t)(Hk / kNumXcd) * max_items + (rest + kNumXcd - 1) / kNumXcd);
 }
 
-// One key block: its first rows and how many there are (>= 1; 64 if more).
-struct Block {
-  const char* k;
-  const char* v;
-  uint32_t kss, vss;   // bytes between rows
-  int rows;
+// The rows of one head in a [rows, heads, 128] tensor, cut into key blocks.
+struct Rows {
+  const char* base;
+  uint32_t ss;         // bytes between rows
+  __device__ Rows(const TensorArg& t, int64_t row0, int head)
+      : base(static_cast<const char*>(t.data) + 2 * (row0 * t.ss + head * t.sh)), ss((uint32_t)(2 * t.ss)) {}
+  __device__ const char* at(int block) const { return base + (int64_t)block * kBlock * ss; }
 };
+
+// The values of a V fragment that are not finite: kind -1 leaves them out, kinds 0, 1, 2 give ones in the places of
+// +inf, -inf and NaN and zeros elsewhere.
+template <bool BF16>
+__device__ inline typename Type<BF16>::vec8 pick(typename Type<BF16>::vec8 v, int kind) {
+  using T = Type<BF16>;
+  i32x4 w = __builtin_bit_cast(i32x4, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    uint32_t out = 0;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t x = ((uint32_t)w[e] >> (16 * half)) & 0xffffu, size = x & 0x7fffu;
+      const int is = size < T::kInf ? -1 : size > T::kInf ? 2 : (int)(x >> 15);
+      const uint32_t keep = is < 0 ? x : T::kOne;
+      out |= (is == kind ? keep : 0u) << (16 * half);
+    }
+    w[e] = (int)out;
+  }
+  return __builtin_bit_cast(typename T::vec8, w);
+}
 
 template <bool BF16, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -92,8 +115,9 @@ void packed_attn_kernel(PackedArgs a) {
   using T = Type<BF16>;
   using vec8 = typename T::vec8;
   using scalar = typename T::scalar;
-  __shared__ __attribute__((aligned(1024))) char k_s[kTileBytes];
-  __shared__ __attribute__((aligned(1024))) char v_s[kTileBytes];
+  __shared__ __attribute__((aligned(1024))) char k_s[2][kTileBytes];
+  __shared__ __attribute__((aligned(1024))) char v_s[2][kTileBytes];
+  __shared__ int again;
 
   int hk, index;
   if (!packed_slot(a.Hk, a.max_items, &hk, &index)) return;
@@ -109,42 +133,40 @@ void packed_attn_kernel(PackedArgs a) {
   const int row = it.row0 + wave * 32 + l32;
   const bool valid = row < it.rows;
   const int query = row / a.group, qh = hk * a.group + row % a.group;
-  // own keys that this row sees, and the fewest of the tile
+  // own keys that a row sees: this lane's, and the fewest and most of the tile
   const int shift = it.nk - nq + 1;
-  const int seen = !valid ? 0 : a.causal ? min(max(query + shift, 0), it.nk) : it.nk;
-  const int seen_first = a.causal ? min(max(it.row0 / a.group + shift, 0), it.nk) : it.nk;
-  const int last_row = min(it.row0 + 32 * NW, it.rows) - 1;
-  const int seen_last = a.causal ? min(max(last_row / a.group + shift, 0), it.nk) : it.nk;
+  auto sees = [&](int r) { return a.causal ? min(max(r / a.group + shift, 0), it.nk) : it.nk; };
+  const int seen = valid ? sees(row) : 0;
+  const int seen_first = sees(it.row0), seen_last = sees(min(it.row0 + 32 * NW, it.rows) - 1);
   const int prefix = a.pooled && it.k0 >= 0 ? 0 : a.prefix;
   const int pw = prefix / kBlock;                                     // whole prefix blocks
   const int own = (seen_last + kBlock - 1) / kBlock;
+  const int n = it.j1 - it.j0;
+  // leading blocks of this item that every row sees whole
+  const int n_full = min(max(pw + seen_first / kBlock - it.j0, 0), n);
 
-  auto block = [&](int j) {
-    Block x;
+  const Rows kp(a.pk, 0, hk), vp(a.pv, 0, hk), ko(a.k, it.k0, hk), vo(a.v, it.k0, hk);
+  const uint32_t klds = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)&k_s[0][0];
+  const uint32_t vlds = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)&v_s[0][0];
+  // Block x of the item into its buffer: this wave's rows of the tile, 4 per 1 KB load.  Rows past the block's end
+  // read its last row again; they are masked.
+  const int r0 = 4 * wave + (lane >> 4);
+  auto load = [&](bool is_k, int x) {
+    const int j = it.j0 + x;
     const bool mine = j >= pw && j < pw + own;
-    const TensorArg& kt = mine ? a.k : a.pk;
-    const TensorArg& vt = mine ? a.v : a.pv;
-    const int first = mine ? (j - pw) * kBlock : min(j, pw) * kBlock;
-    x.rows = min((mine ? it.nk : prefix) - first, kBlock);
-    const int64_t at = (mine ? it.k0 : 0) + (int64_t)first;
-    x.k = static_cast<const char*>(kt.data) + 2 * (at * kt.ss + hk * kt.sh);
-    x.v = static_cast<const char*>(vt.data) + 2 * (at * vt.ss + hk * vt.sh);
-    x.kss = (uint32_t)(2 * kt.ss);
-    x.vss = (uint32_t)(2 * vt.ss);
-    return x;
-  };
-  const uint32_t klds = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)&k_s[0];
-  const uint32_t vlds = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)&v_s[0];
-  // This wave's rows of a tile: 4 rows per 1 KB load.  Rows past the block's end read its last row again: they
-  // are masked.
-  auto load = [&](uint32_t lds, const char* base, uint32_t ss, int rows, bool is_k) {
+    const int block = mine ? j - pw : min(j, pw);
+    const Rows& t = is_k ? (mine ? ko : kp) : (mine ? vo : vp);
+    const int rows = (mine ? it.nk : prefix) - block * kBlock;
+    const char* from = t.at(block);
+    const uint32_t lds = (is_k ? klds : vlds) + (x & 1) * kTileBytes + wave * 1024;
 #pragma unroll
     for (int u = 0; u < 16 / NW; ++u) {
-      const int r = 4 * (NW * u + wave) + (lane >> 4);
-      const int c = is_k ? k_chunk(r, lane & 15) : v_chunk(r, lane & 15);
-      dma16(lds + (NW * u + wave) * 1024, base, (uint32_t)min(r, rows - 1) * ss + (uint32_t)c * 16);
+      const int r = 4 * NW * u + r0;
+      const uint32_t c = 16 * (is_k ? k_chunk(r, lane & 15) : v_chunk(r, lane & 15));
+      dma16(lds + NW * u * 1024, from, (uint32_t)(rows >= kBlock ? r : min(r, rows - 1)) * t.ss + c);
     }
   };
+  if (n > 0) load(true, 0);
 
   vec8 qf[8];
   {
@@ -175,19 +197,7 @@ void packed_attn_kernel(PackedArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[u][r] = 0.f;
 
-  for (int j = it.j0; j < it.j1; ++j) {
-    const Block x = block(j);
-    const bool mine = j >= pw && j < pw + own;
-    const int first = (j - pw) * kBlock;                        // of an own block
-    const int lim = mine ? seen - first : valid ? x.rows : 0;   // keys of this block that the row sees
-    const bool masked = mine ? first + kBlock > seen_first : x.rows < kBlock;
-    __syncthreads();
-    load(klds, x.k, x.kss, x.rows, true);
-    load(vlds, x.v, x.vss, x.rows, false);
-    CHORUS_WAIT_LDS_TILES();
-    __syncthreads();
-    if (__builtin_amdgcn_ballot_w64(lim > 0) == 0) continue;
-    f32x16 s[2];
+  auto qk = [&](f32x16 (&s)[2], const char* kt) {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -196,21 +206,31 @@ void packed_attn_kernel(PackedArgs a) {
     for (int d = 0; d < 8; ++d)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        s[t] = T::mfma(*reinterpret_cast<const vec8*>(k_s + t * 32 * 256 + k_row_off + (((2 * d + hl) ^ k_sw) << 4)),
+        s[t] = T::mfma(*reinterpret_cast<const vec8*>(kt + t * 32 * 256 + k_row_off + (((2 * d + hl) ^ k_sw) << 4)),
                        qf[d], s[t]);
-    if (masked) {
+  };
+  // keys of block x that this row sees
+  auto limit = [&](int x) {
+    const int j = it.j0 + x;
+    return j >= pw && j < pw + own ? seen - (j - pw) * kBlock : valid ? prefix - min(j, pw) * kBlock : 0;
+  };
+  auto mask = [&](f32x16 (&s)[2], int lim) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * t + 8 * (r >> 2) + 4 * hl + (r & 3) >= lim) s[t][r] = -INFINITY;
-    }
+      for (int r = 0; r < 16; ++r)
+        if (32 * t + 8 * (r >> 2) + 4 * hl + (r & 3) >= lim) s[t][r] = -INFINITY;
+  };
+  auto row_max = [&](const f32x16 (&s)[2]) {
     float mx = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
-    const float m_new = fmaxf(m_run, pair_max(mx) * cl2);
+    return pair_max(mx);
+  };
+  auto rescale = [&](float mx) {
+    const float m_new = fmaxf(m_run, mx * cl2);
     if (__builtin_amdgcn_ballot_w64(m_new > m_run + kRescaleLog2) != 0) {
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
@@ -220,68 +240,135 @@ void packed_attn_kernel(PackedArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[u][r] *= alpha;
     }
-    vec8 pf[2][2];
+  };
+  auto probs = [&](const f32x16 (&s)[2], vec8 (&pf)[2][2]) {
+    float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float p = __builtin_amdgcn_exp2f(s[t][r] * cl2 - m_run);
-        l_run += p;
+        sum += p;
         pf[t][r >> 3][r & 7] = (scalar)p;
       }
+    l_run += sum;
+  };
+  auto fragment = [&](const char* vt, int t, int hh, int u) {
+    const char* lo = vt + (32 * t + 16 * hh) * 256 + v_lane_off + (((4 * u + v_c0) ^ v_sw) << 4);
+    return T::transposed(lo, lo + 8 * 256);
+  };
+  auto pv = [&](const vec8 (&pf)[2][2], const char* vt) {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const char* lo = v_s + (32 * t + 16 * hh) * 256 + v_lane_off + (((4 * u + v_c0) ^ v_sw) << 4);
-          vec8 vf = T::transposed(lo, lo + 8 * 256);
-          if (masked) {
-            // A value that some row does not see may be infinite or NaN, and 0 times it is NaN.  Such values are
-            // left out of the product, and what they do to the rows that do see them follows from a product
-            // with their places: a row with a weight on one gets its infinity or NaN.
-            i32x4 w = __builtin_bit_cast(i32x4, vf);
-            uint32_t odd = 0, at[4];
+        for (int u = 0; u < 4; ++u) o[u] = T::mfma(fragment(vt, t, hh, u), pf[t][hh], o[u]);
+  };
+
+  if (n > 0) {
+    f32x16 s0[2], s1[2];
+    float mx;
+    if (tid == 0) again = 0;
+    __builtin_amdgcn_s_waitcnt(0xF70);   // vmcnt(0)
+    __syncthreads();
+    if (n > 1) load(true, 1);
+    load(false, 0);
+    qk(s0, k_s[0]);
+    if (n_full == 0) mask(s0, limit(0));
+    mx = row_max(s0);
+
+    // Block x: its softmax beside QK^T of block x + 1, then PV.
+    auto fused = [&](int x, int par, f32x16 (&sc)[2], f32x16 (&sn)[2]) {
+      CHORUS_WAIT_LDS_TILES();
+      __syncthreads();
+      if (x + 2 < n) load(true, x + 2);
+      load(false, x + 1);
+      rescale(mx);
+      vec8 pf[2][2];
+      qk(sn, k_s[par ^ 1]);
+      probs(sc, pf);
+      pv(pf, v_s[par]);
+      mx = row_max(sn);
+    };
+    int x = 0;
+    for (; x + 2 < n_full; x += 2) {
+      fused(x, 0, s0, s1);
+      fused(x + 1, 1, s1, s0);
+    }
+    // The blocks that need a mask, and up to two ahead of them.
+    for (; x < n; ++x) {
+      const int par = x & 1;
+      CHORUS_WAIT_LDS_TILES();
+      __syncthreads();
+      if (x + 2 < n) load(true, x + 2);
+      if (x + 1 < n) load(false, x + 1);
+      rescale(mx);
+      vec8 pf[2][2];
+      probs(s0, pf);
+      pv(pf, v_s[par]);
+      if (x + 1 < n) {
+        qk(s0, k_s[par ^ 1]);
+        if (x + 1 >= n_full) mask(s0, limit(x + 1));
+        mx = row_max(s0);
+      }
+    }
+
+    // A value that some row of the tile does not see may be infinite or NaN, and its weight 0 times that is NaN.
+    // Where that may have happened the item is done again, more slowly: such values are left out of PV, and a row
+    // gets their infinities and NaN where it has a weight on one, by a product of the weights with their places.
+    if (n_full < n) {
+      float zero = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              at[e] = (((uint32_t)w[e] & T::kExp) + T::kLow) & 0x80008000u;
-              odd |= at[e];
-            }
-            if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
-              i32x4 kind[3];
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t full = (at[e] >> 15) * 0xffffu, word = (uint32_t)w[e];
-                uint32_t is_nan = 0, is_neg = 0;
+        for (int r = 0; r < 16; ++r) zero += o[u][r] * 0.f;
+      if (__builtin_amdgcn_ballot_w64(!(zero == 0.f)) != 0) again = 1;
+      __syncthreads();
+      if (again) {
+        m_run = -FLT_MAX;
+        l_run = 0.f;
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                  const uint32_t x16 = (word >> (16 * half)) & 0xffffu;
-                  if ((x16 & 0x7fffu) > (T::kExp & 0x7fffu)) is_nan |= 0xffffu << (16 * half);
-                  if (x16 & 0x8000u) is_neg |= 0xffffu << (16 * half);
-                }
-                const uint32_t ones = T::kOne * 0x10001u;
-                kind[0][e] = (int)(ones & full & ~is_nan & ~is_neg);
-                kind[1][e] = (int)(ones & full & ~is_nan & is_neg);
-                kind[2][e] = (int)(ones & full & is_nan);
-                w[e] = (int)(word & ~full);
-              }
-              vf = __builtin_bit_cast(vec8, w);
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-              for (int c = 0; c < 3; ++c) {
-                const float what = c == 0 ? INFINITY : c == 1 ? -INFINITY : __builtin_nanf("");
-                f32x16 hit;
+          for (int r = 0; r < 16; ++r) o[u][r] = 0.f;
+#pragma unroll 1
+        for (x = 0; x < n; ++x) {
+          const int par = x & 1;
+          load(true, x);
+          load(false, x);
+          CHORUS_WAIT_LDS_TILES();
+          __syncthreads();
+          vec8 pf[2][2];
+          qk(s0, k_s[par]);
+          if (x >= n_full) mask(s0, limit(x));
+          rescale(row_max(s0));
+          probs(s0, pf);
+          if (x < n_full) {
+            pv(pf, v_s[par]);
+            continue;
+          }
+#pragma unroll 1
+          for (int kind = -1; kind < 3; ++kind) {
+            const float what = kind < 1 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
+            int from = par * kTileBytes;
+            asm volatile("" : "+v"(from));   // read again each time: kept across the kinds the fragments would spill
 #pragma unroll
-                for (int r = 0; r < 16; ++r) hit[r] = 0.f;
-                hit = T::mfma(__builtin_bit_cast(vec8, kind[c]), pf[t][hh], hit);
+            for (int u = 0; u < 4; ++u) {
+              f32x16 hit;
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                  if (hit[r] > 0.f) o[u][r] += what;
-              }
+              for (int r = 0; r < 16; ++r) hit[r] = kind < 0 ? o[u][r] : 0.f;
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) hit = T::mfma(pick<BF16>(fragment(v_s[0] + from, t, hh, u), kind), pf[t][hh], hit);
+#pragma unroll
+              for (int r = 0; r < 16; ++r) o[u][r] = kind < 0 ? hit[r] : hit[r] > 0.f ? o[u][r] + what : o[u][r];
             }
           }
-          o[u] = T::mfma(vf, pf[t][hh], o[u]);
         }
+      }
+    }
   }
 
   const float l_tot = pair_sum(l_run);
