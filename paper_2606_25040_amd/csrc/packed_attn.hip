@@ -121,8 +121,9 @@ void packed_attn_kernel(PackedArgs a) {
 
   int hk, index;
   if (!packed_slot(a.Hk, a.max_items, &hk, &index)) return;
-  if (a.plan.header[kPlanKey] != a.key || index >= a.plan.header[kPlanItems]) return;
+  // read together: an item behind the plan's last is within the buffer
   const PackedItem it = a.plan.items[index];
+  if (a.plan.header[kPlanKey] != a.key || index >= a.plan.header[kPlanItems]) return;
   const int nq = it.rows / a.group;
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -404,37 +405,62 @@ void packed_attn_kernel(PackedArgs a) {
 }
 
 // Joins a tile's pieces: with m the largest of their maxima, O = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.
-// 32 lanes per row.
+// 32 lanes per row, a workgroup for 8 rows at a time; the maxima of up to 32 pieces are read at once.
 template <bool BF16, int NW>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   using scalar = typename Type<BF16>::scalar;
+  constexpr int kTile = 32 * NW, kGroups = kTile / 8;
   const int* header = a.plan.header;
-  if (header[kPlanKey] != a.key || (int)blockIdx.x >= header[kPlanJoins]) return;
-  const PackedJoin jn = a.plan.joins[blockIdx.x];
-  const int hk = blockIdx.y, lane = threadIdx.x & 31;
-  const int np = header[kPlanPrefixPieces], n = jn.pieces + np;
-  constexpr int kTile = 32 * NW;
-  for (int r = threadIdx.x >> 5; r < kTile && jn.row0 + r < jn.rows; r += 8) {
+  if (header[kPlanKey] != a.key) return;
+  const int np = header[kPlanPrefixPieces], first_row = header[kPlanFirstRow];
+  // the first rows of every tile first: the tiles of single tokens have no others
+  const int64_t tiles = (int64_t)header[kPlanJoins] * a.Hk;
+  const int lane = threadIdx.x & 31;
+  for (int64_t w = blockIdx.x; w < tiles * kGroups; w += gridDim.x) {
+    const int r = (int)(w / tiles) * 8 + (threadIdx.x >> 5);
+    const int hk = (int)(w % a.Hk);
+    const PackedJoin jn = a.plan.joins[w % tiles / a.Hk];
     const int row = jn.row0 + r;
-    const int pooled = jn.q0 * a.group - header[kPlanFirstRow] + row;   // among the rows of all sequences
+    if (row >= jn.rows) continue;
+    const int n = jn.pieces + np;
+    const int pooled = jn.q0 * a.group - first_row + row;   // among the rows of all sequences
     auto at = [&](int i) {
       const int64_t slot = i < jn.pieces ? jn.slot + i : pooled / kTile * np + (i - jn.pieces);
       return (slot * a.Hk + hk) * kTile + (i < jn.pieces ? r : pooled % kTile);
     };
     float m = -FLT_MAX;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, a.part_ml[2 * at(i)]);
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, a.part_ml[2 * at(i)]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 32));
     float l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < n; ++i) {
-      const int64_t p = at(i);
-      const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - m);
-      const float4 v = *reinterpret_cast<const float4*>(a.part_o + p * kHeadDim + 4 * lane);
-      l += f * a.part_ml[2 * p + 1];
-      o.x += f * v.x;
-      o.y += f * v.y;
-      o.z += f * v.z;
-      o.w += f * v.w;
+    for (int base = 0; base < n; base += 32) {
+      const int mine = base + lane;
+      float f = 0.f;
+      if (mine < n) {
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * at(mine));
+        f = __builtin_amdgcn_exp2f(ml.x - m);
+        l += f * ml.y;
+      }
+      const int some = min(n - base, 32);
+      for (int i = 0; i < some; i += 4) {   // four loads in flight
+        float4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = i + e < some ? *reinterpret_cast<const float4*>(a.part_o + at(base + i + e) * kHeadDim + 4 * lane)
+                              : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float fi = __shfl(f, i + e, 32);
+          o.x += fi * v[e].x;
+          o.y += fi * v[e].y;
+          o.z += fi * v[e].z;
+          o.w += fi * v[e].w;
+        }
+      }
     }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) l += __shfl_xor(l, d, 32);
     const bool empty = l == 0.f;
     const float inv_l = empty ? 0.f : 1.f / l;
     const int query = jn.q0 + row / a.group, qh = hk * a.group + row % a.group;
@@ -452,7 +478,8 @@ template <bool BF16, int NW>
 void launch_packed(const PackedConfig& c, const PackedArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((packed_attn_kernel<BF16, NW>), dim3((unsigned)packed_grid(a.Hk, c.max_items)), dim3(64 * NW), 0, st,
                      a);
-  hipLaunchKernelGGL((packed_join_kernel<BF16, NW>), dim3(c.max_joins, a.Hk), dim3(256), 0, st, a);
+  const int64_t groups = (int64_t)c.max_joins * a.Hk * (32 * NW / 8);
+  hipLaunchKernelGGL((packed_join_kernel<BF16, NW>), dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, a);
 }
 
 }  // namespace

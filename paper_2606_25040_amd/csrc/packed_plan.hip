@@ -97,18 +97,22 @@ struct Tile {
   int row0, rows, blocks;
 };
 
-__device__ inline Tile tile_at(const PlanArgs& a, int t) {
+// Up to this many sequences are kept in LDS, more in the plan buffer.
+constexpr int kNear = 1024;
+
+template <class Seqs>
+__device__ inline Tile tile_at(const PlanArgs& a, const Seqs& seqs, int t) {
   int lo = 0, hi = a.n_seqs;   // the last sequence whose first tile is at or before t
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (a.plan.seqs[mid].tile0 <= t)
+    if (seqs[mid].tile0 <= t)
       lo = mid;
     else
       hi = mid;
   }
   Tile x;
-  x.seq = a.plan.seqs[lo];
-  const int nq = a.plan.seqs[lo + 1].q0 - x.seq.q0;
+  x.seq = seqs[lo];
+  const int nq = seqs[lo + 1].q0 - x.seq.q0;
   x.rows = nq * a.group;
   x.row0 = (t - x.seq.tile0) * a.tile;
   int seen = x.seq.nk;
@@ -120,18 +124,37 @@ __device__ inline Tile tile_at(const PlanArgs& a, int t) {
   return x;
 }
 
+template <bool NEAR>
 __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   __shared__ int wave_s[kThreads / 64];
   __shared__ unsigned long long cost_s;
   __shared__ int flags_s, class_s[kClasses];
+  __shared__ PackedSeq near_s[NEAR ? kNear + 1 : 1];
+  PackedSeq* far = a.plan.seqs;
+  auto seqs = [&]() -> auto& {
+    if constexpr (NEAR)
+      return near_s;
+    else
+      return far;
+  };
+  auto& seq = seqs();
   const int tid = threadIdx.x, N = a.n_seqs;
   if (tid == 0) {
     cost_s = 0;
     flags_s = 0;
   }
   if (tid < kClasses) class_s[tid] = 0;
-  __syncthreads();
-
+  // key rows first: their loads are in flight during the first scan
+  int flags = 0;
+  for (int i = tid; i < N; i += kThreads) {
+    const int raw0 = a.k_offsets[i];
+    const int64_t raw = a.k_lens ? a.k_lens[i] : (int64_t)a.k_offsets[i + 1] - raw0;
+    const int k0 = min(max(raw0, 0), a.total_k);
+    const int nk = (int)min(max(raw, (int64_t)0), (int64_t)(a.total_k - k0));
+    if (k0 != raw0 || nk != raw) flags |= 2;
+    seq[i].k0 = k0;
+    seq[i].nk = nk;
+  }
   int run = 0, total;
   for (int base = 0; base <= N; base += kThreads) {
     const int i = base + tid;
@@ -139,46 +162,40 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
     const int v = max(run, block_scan(min(max(raw, 0), a.total_q), Max(), wave_s, &total));
     run = max(run, total);
     if (i <= N) {
-      a.plan.seqs[i].q0 = v;
-      if (v != raw) atomicOr(&flags_s, 1);
+      seq[i].q0 = v;
+      if (v != raw) flags |= 1;
     }
   }
+  if (flags) atomicOr(&flags_s, flags);
   __syncthreads();
   run = 0;
   for (int base = 0; base < N; base += kThreads) {
     const int i = base + tid;
     int tiles = 0;
     if (i < N) {
-      const int64_t rows = (int64_t)(a.plan.seqs[i + 1].q0 - a.plan.seqs[i].q0) * a.group;
+      const int64_t rows = (int64_t)(seq[i + 1].q0 - seq[i].q0) * a.group;
       tiles = (int)((rows + a.tile - 1) / a.tile);
     }
     const int upto = run + block_scan(tiles, Add(), wave_s, &total);
     run += total;
-    if (i < N) {
-      const int raw0 = a.k_offsets[i];
-      const int64_t raw = a.k_lens ? a.k_lens[i] : (int64_t)a.k_offsets[i + 1] - raw0;
-      const int k0 = min(max(raw0, 0), a.total_k);
-      const int nk = (int)min(max(raw, (int64_t)0), (int64_t)(a.total_k - k0));
-      if (k0 != raw0 || nk != raw) atomicOr(&flags_s, 2);
-      a.plan.seqs[i].tile0 = upto - tiles;
-      a.plan.seqs[i].k0 = k0;
-      a.plan.seqs[i].nk = nk;
-    }
+    if (i < N) seq[i].tile0 = upto - tiles;
   }
   const int n_tiles = run;
   __syncthreads();
 
-  const int first = a.plan.seqs[0].q0;
-  const int pooled_rows = (a.plan.seqs[N].q0 - first) * a.group;
+  const int first = seq[0].q0;
+  const int pooled_rows = (seq[N].q0 - first) * a.group;
   const int pooled_tiles = a.pooled ? (pooled_rows + a.tile - 1) / a.tile : 0;
   const int prefix_blocks = (a.prefix + kBlock - 1) / kBlock;
-  unsigned long long cost = 0;
-  for (int t = tid; t < n_tiles; t += kThreads) cost += tile_at(a, t).blocks;
+  // this thread's first tile is kept; most plans have no second
+  const Tile mine = tid < n_tiles ? tile_at(a, seq, tid) : Tile{};
+  unsigned long long cost = mine.blocks;
+  for (int t = tid + kThreads; t < n_tiles; t += kThreads) cost += tile_at(a, seq, t).blocks;
   if (cost) atomicAdd(&cost_s, cost);
   __syncthreads();
   cost = cost_s + (unsigned long long)pooled_tiles * prefix_blocks;
-  const int chunk = (int)min((cost + a.per_head - 1) / a.per_head + 0ull, (unsigned long long)(1 << 26));
-  const int piece = max(chunk, kMinChunk), longest = piece + piece / 2;
+  const int piece = max((int)min((cost + a.per_head - 1) / a.per_head, 1ull << 26), kMinChunk);
+  const int longest = piece + piece / 2;
   auto pieces = [&](int blocks) { return blocks > longest ? (blocks + piece - 1) / piece : 1; };
   auto class_of = [&](int blocks, int p) {
     return kClasses - 1 - (int)((int64_t)((blocks + p - 1) / p) * kClasses / (longest + 1));
@@ -186,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   const int np = pooled_tiles ? pieces(prefix_blocks) : 0;
 
   for (int t = tid; t < n_tiles; t += kThreads) {
-    const int n = tile_at(a, t).blocks, p = pieces(n);
+    const int n = t < kThreads ? mine.blocks : tile_at(a, seq, t).blocks, p = pieces(n);
     if (n > 0 || !a.pooled) atomicAdd(&class_s[class_of(n, p)], p);
   }
   if (tid == 0 && np) atomicAdd(&class_s[class_of(prefix_blocks, np)], pooled_tiles * np);
@@ -216,7 +233,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
     Tile x = {};
     int p = 0, own = 0, joined = 0;
     if (t < n_tiles) {
-      x = tile_at(a, t);
+      x = base ? tile_at(a, seq, t) : mine;
       p = a.pooled && x.blocks == 0 ? 0 : pieces(x.blocks);
       joined = a.pooled || p > 1;
       own = joined ? p : 0;
@@ -226,10 +243,11 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
     const int join = joins + block_scan(joined, Add(), wave_s, &join_total) - joined;
     slots += slot_total;
     joins += join_total;
-    for (int i = 0; i < p; ++i) {
-      const int at = atomicAdd(&class_s[class_of(x.blocks, p)], 1);
-      a.plan.items[at] = {x.seq.q0, x.row0, x.rows, (int)((int64_t)i * x.blocks / p),
-                          (int)((int64_t)(i + 1) * x.blocks / p), x.seq.k0, x.seq.nk, joined ? slot + i : -1};
+    if (p) {
+      int at = atomicAdd(&class_s[class_of(x.blocks, p)], p);
+      for (int i = 0; i < p; ++i, ++at)
+        a.plan.items[at] = {x.seq.q0, x.row0, x.rows, (int)((int64_t)i * x.blocks / p),
+                            (int)((int64_t)(i + 1) * x.blocks / p), x.seq.k0, x.seq.nk, joined ? slot + i : -1};
     }
     if (joined) a.plan.joins[join] = {x.seq.q0, x.row0, x.rows, slot, p, {0, 0, 0}};
   }
@@ -248,7 +266,10 @@ hipError_t launch_packed_plan(const chorus_packed_shape& s, const PackedConfig& 
                               const int32_t* k_offsets, const int32_t* k_lens, const PackedPlan& plan, hipStream_t st) {
   const PlanArgs a = {q_offsets, k_offsets, k_lens,   plan,       s.n_seqs, s.total_q,  s.total_k, s.prefix,
                       s.q_heads / s.kv_heads, s.causal, 32 * c.waves, c.pooled, c.per_head, c.key};
-  hipLaunchKernelGGL(packed_plan_kernel, dim3(1), dim3(kThreads), 0, st, a);
+  if (s.n_seqs <= kNear)
+    hipLaunchKernelGGL((packed_plan_kernel<true>), dim3(1), dim3(kThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((packed_plan_kernel<false>), dim3(1), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 

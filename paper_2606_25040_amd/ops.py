@@ -614,21 +614,27 @@ class VisitMap:
         return bits.reshape(w.shape[0], -1)[:, : self.n_kv]
 
 
-def _current(*tensors) -> None:
-    """Every given tensor lives on the current device, whose stream the call is put on."""
+def _current(*tensors) -> int:
+    """Every given tensor lives on the current device; returns that device's current stream, which the call is put on."""
+    here = None
     for t in tensors:
         if t is None:
             continue
         if not t.is_cuda:
             raise ValueError("expected a device tensor")
-        if t.device.index != torch.cuda.current_device():
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+        if here is None:
+            here = torch.cuda.current_device()
+        if t.get_device() != here:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+    return torch._C._cuda_getCurrentRawStream(here)
 
 
 def _writable(t: torch.Tensor, name: str) -> None:
     """Rows of an output do not share memory: each stride reaches past what the smaller ones span."""
+    if t.is_contiguous():
+        return
     reach = 1
-    for size, stride in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n > 1), key=lambda x: x[1]):
+    for stride, size in sorted((s, n) for n, s in zip(t.shape, t.stride()) if n > 1):
         if stride < reach:
             raise ValueError(f"{name} has rows that share memory")
         reach = stride * (size - 1) + reach
@@ -668,7 +674,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None = None, rotary: RotaryA
     L = load_library()
     if norm not in _NORMS:
         raise ValueError("norm must be None, 'head' or 'token'")
-    _current(q, k, positions, q_weight, k_weight, q_out, k_out)
+    stream = _current(q, k, positions, q_weight, k_weight, q_out, k_out)
     dt = _dtype_code(q)
     if q.dim() != 4:
         raise ValueError("expected a [B, S, H, D] tensor")
@@ -700,18 +706,19 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None = None, rotary: RotaryA
         q_out = torch.empty((B, S, H, D), dtype=q.dtype, device=q.device)
     elif q_out.shape != q.shape or q_out.dtype != q.dtype:
         raise ValueError("q_out must have q's shape and dtype")
+    else:
+        _writable(q_out, "q_out")
     if k is not None and k_out is None:
         k_out = torch.empty((B, S, Hk, D), dtype=k.dtype, device=k.device)
     elif k is not None and (k_out.shape != k.shape or k_out.dtype != k.dtype):
         raise ValueError("k_out must have k's shape and dtype")
-    _writable(q_out, "q_out")
-    if k is not None:
+    elif k is not None:
         _writable(k_out, "k_out")
     st = L.chorus_qk_norm_rope(dt, ctypes.byref(_shape(q)), Hk, ctypes.byref(_tensor(q)),
                                None if k is None else ctypes.byref(_tensor(k)), _NORMS[norm], _ptr(q_weight),
                                _ptr(k_weight), float(eps), None if rotary is None else ctypes.byref(rotary.c),
                                _ptr(positions), axis_stride, batch_stride, ctypes.byref(_tensor(q_out)),
-                               None if k is None else ctypes.byref(_tensor(k_out)), _stream())
+                               None if k is None else ctypes.byref(_tensor(k_out)), stream)
     _check(st, "chorus_qk_norm_rope")
     return q_out if k is None else (q_out, k_out)
 
@@ -721,6 +728,10 @@ class PackedPlan:
     """Work plan of a batch of packed sequences (chorus_plan_packed_attn), for every layer of a step."""
     data: torch.Tensor       # uint8; the plan starts at its first 256-byte boundary
     shape: PackedShape
+
+    def __post_init__(self):
+        self.workspace_bytes = load_library().chorus_packed_attn_workspace_size(ctypes.byref(self.shape))
+        self.plan_bytes = load_library().chorus_packed_plan_bytes(ctypes.byref(self.shape))
 
     def flags(self) -> int:
         """Synchronises; 0, or 1 (q_offsets) | 2 (k_offsets, k_lens) where offsets or lengths had to be clamped."""
@@ -737,7 +748,7 @@ def plan_packed_attn(q_offsets: torch.Tensor, k_offsets: torch.Tensor, total_q: 
     ``k_lens`` [N].  ``prefix``: rows of a prefix that every sequence sees.  ``max_q``: the longest sequence's
     queries, if known.  ``out``: a plan of the same shape to write again."""
     L = load_library()
-    _current(q_offsets, k_offsets, k_lens)
+    stream = _current(q_offsets, k_offsets, k_lens, None if out is None else out.data)
     N = q_offsets.numel() - 1
     for t, name in ((q_offsets, "q_offsets"), (k_offsets, "k_offsets"), (k_lens, "k_lens")):
         if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous()):
@@ -746,24 +757,25 @@ def plan_packed_attn(q_offsets: torch.Tensor, k_offsets: torch.Tensor, total_q: 
         raise ValueError("q_offsets holds N + 1 entries, k_offsets N + 1 (N with k_lens), k_lens N")
     shape = PackedShape(N, int(total_q), int(total_k), int(prefix), int(q_heads), int(kv_heads), 128, int(bool(causal)),
                         int(max_q))
-    need = L.chorus_packed_plan_bytes(ctypes.byref(shape))
     if out is None:
+        need = L.chorus_packed_plan_bytes(ctypes.byref(shape))
         out = PackedPlan(torch.empty(need + 256, dtype=torch.uint8, device=q_offsets.device), shape)
     elif bytes(out.shape) != bytes(shape):
         raise ValueError("out is a plan of another shape")
-    _current(out.data)
     st = L.chorus_plan_packed_attn(ctypes.byref(shape), q_offsets.data_ptr(), k_offsets.data_ptr(), _ptr(k_lens),
-                                   _aligned(out.data), need, _stream())
+                                   _aligned(out.data), out.plan_bytes, stream)
     _check(st, "chorus_plan_packed_attn")
     return out
 
 
-def _rows(t: torch.Tensor, rows: int, heads: int, like: torch.Tensor, name: str) -> Tensor:
-    if t.dim() != 3 or tuple(t.shape) != (rows, heads, like.shape[-1]) or t.dtype != like.dtype:
-        raise ValueError(f"{name} must be a {like.dtype} [{rows}, {heads}, {like.shape[-1]}] tensor")
-    if t.stride(2) != 1:
+def _rows(t: torch.Tensor, rows: int, heads: int, like: torch.Tensor, name: str):
+    """Pointer to a chorus_tensor of a [rows, heads, 128] tensor."""
+    if t.shape != (rows, heads, 128) or t.dtype != like.dtype:
+        raise ValueError(f"{name} must be a {like.dtype} [{rows}, {heads}, 128] tensor")
+    ss, sh, sd = t.stride()
+    if sd != 1:
         raise ValueError("head dim must be contiguous")
-    return Tensor(t.data_ptr(), 0, t.stride(0), t.stride(1))
+    return ctypes.byref(Tensor(t.data_ptr(), 0, ss, sh))
 
 
 def packed_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: PackedPlan, sm_scale: float | None = None,
@@ -773,25 +785,24 @@ def packed_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Pac
     ``prefix_k, prefix_v [prefix, kv_heads, 128]``) by ``plan``; f16 or bf16.  Returns ``out`` (and ``lse [q_heads,
     total_q]`` fp32 when ``return_lse``); rows of no sequence are not written."""
     L = load_library()
-    _current(q, k, v, prefix_k, prefix_v, out, plan.data)
+    stream = _current(q, k, v, prefix_k, prefix_v, out, plan.data)
     s = plan.shape
     dt = _dtype_code(q)
     if (prefix_k is None) != (s.prefix == 0) or (prefix_v is None) != (s.prefix == 0):
         raise ValueError(f"the plan's prefix has {s.prefix} rows")
+    ct = [_rows(q, s.total_q, s.q_heads, q, "q"), _rows(k, s.total_k, s.kv_heads, q, "k"),
+          _rows(v, s.total_k, s.kv_heads, q, "v"), None, None]
+    if s.prefix:
+        ct[3:] = _rows(prefix_k, s.prefix, s.kv_heads, q, "prefix_k"), _rows(prefix_v, s.prefix, s.kv_heads, q, "prefix_v")
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    ct = [_rows(q, s.total_q, s.q_heads, q, "q"), _rows(k, s.total_k, s.kv_heads, q, "k"),
-          _rows(v, s.total_k, s.kv_heads, q, "v")]
-    ct += [_rows(t, s.prefix, s.kv_heads, q, n) if s.prefix else None for t, n in ((prefix_k, "prefix_k"),
-                                                                                  (prefix_v, "prefix_v"))]
-    co = _rows(out, s.total_q, s.q_heads, q, "out")
-    _writable(out, "out")
+    else:
+        _writable(out, "out")
     lse = torch.empty((s.q_heads, s.total_q), dtype=torch.float32, device=q.device) if return_lse else None
-    sm = 1.0 / math.sqrt(q.shape[-1]) if sm_scale is None else float(sm_scale)
-    need = L.chorus_packed_attn_workspace_size(ctypes.byref(s))
-    ws = _workspace(need, q.device)
-    st = L.chorus_packed_attn_fwd(dt, ctypes.byref(s), *(None if t is None else ctypes.byref(t) for t in ct), sm,
-                                  _aligned(plan.data), plan.data.numel() - 256, ctypes.byref(co), _ptr(lse),
-                                  _aligned(ws), need, _stream())
+    sm = 128 ** -0.5 if sm_scale is None else float(sm_scale)
+    ws = _workspace(plan.workspace_bytes, q.device)
+    st = L.chorus_packed_attn_fwd(dt, ctypes.byref(s), *ct, sm, _aligned(plan.data), plan.plan_bytes,
+                                  _rows(out, s.total_q, s.q_heads, q, "out"), _ptr(lse), _aligned(ws),
+                                  plan.workspace_bytes, stream)
     _check(st, "chorus_packed_attn_fwd")
     return (out, lse) if return_lse else out
