@@ -517,8 +517,9 @@ chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t
  *                 positions[a * pos_stride_axis + b * pos_stride_b + s]
  *                 (strides >= 0; pos_stride_b = 0 shares them); any value.
  * q_out, k_out  : as q and k; the same tensor as the input (same pointer and
- *                 strides) for in place, otherwise they must not overlap it.
- * CHORUS_NORM_TOKEN supports up to 128 heads; B * S * heads < 2^31.
+ *                 strides) for in place, otherwise their spans of memory must
+ *                 not overlap.
+ * CHORUS_NORM_TOKEN supports up to 128 heads; B * S * heads <= 2^30.
  * ------------------------------------------------------------------------- */
 typedef enum { CHORUS_NORM_NONE = 0, CHORUS_NORM_HEAD = 1, CHORUS_NORM_TOKEN = 2 } chorus_norm;
 

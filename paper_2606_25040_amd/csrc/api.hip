@@ -738,8 +738,8 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
     a.adjacent = rotary->adjacent;
   }
   const int64_t heads = std::max(shape->H, kv_heads);
-  if ((int64_t)shape->B * shape->S > INT32_MAX / heads)
-    return fail(CHORUS_ERR_UNSUPPORTED, "B * S * heads exceeds 2^31");
+  if ((int64_t)shape->B * shape->S > (1 << 30) / heads)
+    return fail(CHORUS_ERR_UNSUPPORTED, "B * S * heads exceeds 2^30");
   if ((!same_tensor(q, q_out) && spans_overlap(q, shape->H, q_out, shape->H, shape->B, shape->S)) ||
       (k && ((!same_tensor(k, k_out) && spans_overlap(k, kv_heads, k_out, kv_heads, shape->B, shape->S)))))
     return fail(CHORUS_ERR_INVALID_ARG, "an output overlaps its input without being the same tensor");
@@ -876,6 +876,11 @@ chorus_status chorus_packed_attn_fwd(chorus_dtype dtype, const chorus_packed_sha
   a.prefix = shape->prefix;
   a.Hk = shape->kv_heads;
   a.group = shape->q_heads / shape->kv_heads;
+  // with 2^(l - 1) < group <= 2^l: ceil(2^(31 + l) / group) < 2^32 is within 1 / 2^(31 + l) * group of exact
+  int l = 0;
+  while ((1ll << l) < a.group) ++l;
+  a.group_shift = 31 + l;
+  a.group_mul = (uint32_t)(((1ull << (31 + l)) + a.group - 1) / a.group);
   a.causal = shape->causal;
   a.pooled = c.pooled;
   a.max_items = c.max_items;

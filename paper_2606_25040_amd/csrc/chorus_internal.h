@@ -140,8 +140,9 @@ struct RopeArgs {
   int pairs[4];
   int adjacent;
   double freqs[kHeadDim / 2];
+  int streamed;            // set by the launch
 };
-hipError_t launch_qk_norm_rope(chorus_dtype dt, const RopeArgs& a, hipStream_t st);
+hipError_t launch_qk_norm_rope(chorus_dtype dt, RopeArgs a, hipStream_t st);
 
 // ---- attention over packed sequences (packed_plan.hip, packed_attn.hip) ----
 // How a shape is cut, from host-known sizes only; the same for the plan and
@@ -189,6 +190,7 @@ struct PackedArgs {
   float* part_o;           // [slot][key head][row][128]
   float* part_ml;          // [slot][key head][row][2]: running maximum (log2), sum
   int total_q, prefix, Hk, group, causal, pooled;
+  uint32_t group_mul, group_shift;   // x / group = x * group_mul >> group_shift for 0 <= x < 2^31
   int max_items;
   int32_t key;
   float sm_scale;
