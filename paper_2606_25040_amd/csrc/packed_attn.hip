@@ -33,7 +33,6 @@ template <>
 struct Type<true> {
   using vec8 = bf16x8;
   using scalar = __bf16;
-  static constexpr uint32_t kInf = 0x7f80u, kOne = 0x3f80u;
   static __device__ inline f32x16 mfma(vec8 a, vec8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -47,7 +46,6 @@ template <>
 struct Type<false> {
   using vec8 = f16x8;
   using scalar = _Float16;
-  static constexpr uint32_t kInf = 0x7c00u, kOne = 0x3c00u;
   static __device__ inline f32x16 mfma(vec8 a, vec8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
@@ -59,24 +57,27 @@ struct Type<false> {
 };
 
 // Key head and item of a workgroup.  Workgroups go round the 8 XCDs; XCD x takes key heads x, x + 8, ..., one
-// after the other, so the items in flight on it share one head's keys in its L2, and the heads beyond the last
-// multiple of 8 are dealt to all XCDs item by item.
+// after the other (blockIdx.y), so the items in flight on it share one head's keys in its L2, and the heads beyond the
+// last multiple of 8 are dealt to all XCDs item by item.
 __device__ inline bool packed_slot(int Hk, int max_items, int* head, int* item) {
-  const int x = blockIdx.x % kNumXcd, k = blockIdx.x / kNumXcd;
-  const int rounds = Hk / kNumXcd, rest = Hk % kNumXcd;
-  if (k < rounds * max_items) {
-    *head = k / max_items * kNumXcd + x;
-    *item = k % max_items;
-    return true;
+  const int x = blockIdx.x, y = blockIdx.y, rounds = Hk / kNumXcd, rest = Hk % kNumXcd;
+  if (y < rounds) {
+    *head = kNumXcd * y + x % kNumXcd;
+    *item = x / kNumXcd;
+  } else {
+    *head = kNumXcd * y + x % rest;
+    *item = x / rest;
   }
-  const int left = (k - rounds * max_items) * kNumXcd + x;
-  *head = rounds * kNumXcd + left % rest;
-  *item = left / rest;
   return *item < max_items;
 }
-inline int64_t packed_grid(int Hk, int max_items) {
-  const int64_t rest = (int64_t)(Hk % kNumXcd) * max_items;
-  return kNumXcd * ((int64_t)(Hk / kNumXcd) * max_items + (rest + kNumXcd - 1) / kNumXcd);
+inline dim3 packed_grid(int Hk, int max_items) {
+  const int rounds = Hk / kNumXcd, rest = Hk % kNumXcd;
+  return dim3(rounds ? kNumXcd * max_items : rest * max_items, rounds + (rest > 0));
+}
+
+// row / group
+__device__ inline int in_group(const PackedArgs& a, int row) {
+  return (int)(((uint64_t)(uint32_t)row * a.group_mul) >> a.group_shift);
 }
 
 // The rows of one head in a [rows, heads, 128] tensor, cut into key blocks.
@@ -88,28 +89,7 @@ struct Rows {
   __device__ const char* at(int block) const { return base + (int64_t)block * kBlock * ss; }
 };
 
-// The values of a V fragment that are not finite: kind -1 leaves them out, kinds 0, 1, 2 give ones in the places of
-// +inf, -inf and NaN and zeros elsewhere.
-template <bool BF16>
-__device__ inline typename Type<BF16>::vec8 pick(typename Type<BF16>::vec8 v, int kind) {
-  using T = Type<BF16>;
-  i32x4 w = __builtin_bit_cast(i32x4, v);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    uint32_t out = 0;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const uint32_t x = ((uint32_t)w[e] >> (16 * half)) & 0xffffu, size = x & 0x7fffu;
-      const int is = size < T::kInf ? -1 : size > T::kInf ? 2 : (int)(x >> 15);
-      const uint32_t keep = is < 0 ? x : T::kOne;
-      out |= (is == kind ? keep : 0u) << (16 * half);
-    }
-    w[e] = (int)out;
-  }
-  return __builtin_bit_cast(typename T::vec8, w);
-}
-
-template <bool BF16, int NW>
+template <bool BF16, bool PREFIX, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void packed_attn_kernel(PackedArgs a) {
   using T = Type<BF16>;
@@ -121,10 +101,12 @@ void packed_attn_kernel(PackedArgs a) {
 
   int hk, index;
   if (!packed_slot(a.Hk, a.max_items, &hk, &index)) return;
-  // read together: an item behind the plan's last is within the buffer
-  const PackedItem it = a.plan.items[index];
-  if (a.plan.header[kPlanKey] != a.key || index >= a.plan.header[kPlanItems]) return;
-  const int nq = it.rows / a.group;
+  // read together, with scalar loads; an item behind the plan's last is within the buffer
+  ConstI32* header = as_constant(a.plan.header);
+  ConstI32* words = as_constant(reinterpret_cast<const int32_t*>(a.plan.items + index));
+  const PackedItem it = {words[0], words[1], words[2], words[3], words[4], words[5], words[6], words[7]};
+  if ((header[kPlanKey] != a.key) | (index >= header[kPlanItems])) return;
+  const int nq = in_group(a, it.rows);
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63;
@@ -133,44 +115,51 @@ void packed_attn_kernel(PackedArgs a) {
 
   const int row = it.row0 + wave * 32 + l32;
   const bool valid = row < it.rows;
-  const int query = row / a.group, qh = hk * a.group + row % a.group;
   // own keys that a row sees: this lane's, and the fewest and most of the tile
   const int shift = it.nk - nq + 1;
-  auto sees = [&](int r) { return a.causal ? min(max(r / a.group + shift, 0), it.nk) : it.nk; };
+  auto sees = [&](int r) { return a.causal ? min(max(in_group(a, r) + shift, 0), it.nk) : it.nk; };
   const int seen = valid ? sees(row) : 0;
   const int seen_first = sees(it.row0), seen_last = sees(min(it.row0 + 32 * NW, it.rows) - 1);
-  const int prefix = a.pooled && it.k0 >= 0 ? 0 : a.prefix;
+  const int prefix = !PREFIX || (a.pooled && it.k0 >= 0) ? 0 : a.prefix;
   const int pw = prefix / kBlock;                                     // whole prefix blocks
   const int own = (seen_last + kBlock - 1) / kBlock;
   const int n = it.j1 - it.j0;
   // leading blocks of this item that every row sees whole
   const int n_full = min(max(pw + seen_first / kBlock - it.j0, 0), n);
 
-  const Rows kp(a.pk, 0, hk), vp(a.pv, 0, hk), ko(a.k, it.k0, hk), vo(a.v, it.k0, hk);
+  const Rows ko(a.k, it.k0, hk), vo(a.v, it.k0, hk);
+  const Rows kp(PREFIX ? a.pk : a.k, 0, hk), vp(PREFIX ? a.pv : a.v, 0, hk);
   const uint32_t klds = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)&k_s[0][0];
   const uint32_t vlds = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)&v_s[0][0];
   // Block x of the item into its buffer: this wave's rows of the tile, 4 per 1 KB load.  Rows past the block's end
   // read its last row again; they are masked.
   const int r0 = 4 * wave + (lane >> 4);
-  auto load = [&](bool is_k, int x) {
+  auto load = [&](bool is_k, int x, int buffer) {
     const int j = it.j0 + x;
-    const bool mine = j >= pw && j < pw + own;
+    const bool mine = !PREFIX || (j >= pw && j < pw + own);
     const int block = mine ? j - pw : min(j, pw);
     const Rows& t = is_k ? (mine ? ko : kp) : (mine ? vo : vp);
     const int rows = (mine ? it.nk : prefix) - block * kBlock;
     const char* from = t.at(block);
-    const uint32_t lds = (is_k ? klds : vlds) + (x & 1) * kTileBytes + wave * 1024;
+    const uint32_t lds = (is_k ? klds : vlds) + buffer * kTileBytes + wave * 1024;
+    // both layouts repeat after 16 rows
+    static_assert(4 * NW % 16 == 0, "a lane's chunk is the same in all its rows");
+    const uint32_t c = 16 * (is_k ? k_chunk(r0, lane & 15) : v_chunk(r0, lane & 15));
+    if (rows >= kBlock) {
 #pragma unroll
-    for (int u = 0; u < 16 / NW; ++u) {
-      const int r = 4 * NW * u + r0;
-      const uint32_t c = 16 * (is_k ? k_chunk(r, lane & 15) : v_chunk(r, lane & 15));
-      dma16(lds + NW * u * 1024, from, (uint32_t)(rows >= kBlock ? r : min(r, rows - 1)) * t.ss + c);
+      for (int u = 0; u < 16 / NW; ++u)
+        dma16(lds + NW * u * 1024, from + (int64_t)(4 * NW * u) * t.ss, (uint32_t)r0 * t.ss + c);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 16 / NW; ++u)
+        dma16(lds + NW * u * 1024, from, (uint32_t)min(4 * NW * u + r0, rows - 1) * t.ss + c);
     }
   };
-  if (n > 0) load(true, 0);
+  if (n > 0) load(true, 0, 0);
 
   vec8 qf[8];
   {
+    const int query = in_group(a, row), qh = hk * a.group + row - query * a.group;
     const uint16_t* qp = static_cast<const uint16_t*>(a.q.data) + (int64_t)(it.q0 + query) * a.q.ss +
                          (int64_t)qh * a.q.sh + 8 * hl;
 #pragma unroll
@@ -183,6 +172,9 @@ void packed_attn_kernel(PackedArgs a) {
       }
     }
   }
+  __builtin_amdgcn_sched_barrier(0);   // the loads that may still be on their way come after Q's
+  if (n > 0) load(false, 0, 0);
+  if (n > 1) load(true, 1, 1);
   const int k_row_off = l32 * 256;
   const int k_sw = l32 & 15;
   const int v_lane_off = (j16 >> 2) * 256 + 8 * (j16 & 1) + 4 * (g >> 1) * 256;
@@ -213,7 +205,7 @@ void packed_attn_kernel(PackedArgs a) {
   // keys of block x that this row sees
   auto limit = [&](int x) {
     const int j = it.j0 + x;
-    return j >= pw && j < pw + own ? seen - (j - pw) * kBlock : valid ? prefix - min(j, pw) * kBlock : 0;
+    return !PREFIX || (j >= pw && j < pw + own) ? seen - (j - pw) * kBlock : valid ? prefix - min(j, pw) * kBlock : 0;
   };
   auto mask = [&](f32x16 (&s)[2], int lim) {
 #pragma unroll
@@ -271,20 +263,21 @@ void packed_attn_kernel(PackedArgs a) {
     f32x16 s0[2], s1[2];
     float mx;
     if (tid == 0) again = 0;
-    __builtin_amdgcn_s_waitcnt(0xF70);   // vmcnt(0)
+    // Q and the first K tile have landed; the next K and the first V tile may be on their way
+    if (n > 1)
+      CHORUS_WAIT_VMCNT(8);
+    else
+      CHORUS_WAIT_VMCNT(4);
     __syncthreads();
-    if (n > 1) load(true, 1);
-    load(false, 0);
     qk(s0, k_s[0]);
     if (n_full == 0) mask(s0, limit(0));
     mx = row_max(s0);
 
-    // Block x: its softmax beside QK^T of block x + 1, then PV.
     auto fused = [&](int x, int par, f32x16 (&sc)[2], f32x16 (&sn)[2]) {
       CHORUS_WAIT_LDS_TILES();
       __syncthreads();
-      if (x + 2 < n) load(true, x + 2);
-      load(false, x + 1);
+      if (x + 2 < n) load(true, x + 2, x & 1);
+      load(false, x + 1, (x + 1) & 1);
       rescale(mx);
       vec8 pf[2][2];
       qk(sn, k_s[par ^ 1]);
@@ -297,13 +290,12 @@ void packed_attn_kernel(PackedArgs a) {
       fused(x, 0, s0, s1);
       fused(x + 1, 1, s1, s0);
     }
-    // The blocks that need a mask, and up to two ahead of them.
     for (; x < n; ++x) {
       const int par = x & 1;
       CHORUS_WAIT_LDS_TILES();
       __syncthreads();
-      if (x + 2 < n) load(true, x + 2);
-      if (x + 1 < n) load(false, x + 1);
+      if (x + 2 < n) load(true, x + 2, x & 1);
+      if (x + 1 < n) load(false, x + 1, (x + 1) & 1);
       rescale(mx);
       vec8 pf[2][2];
       probs(s0, pf);
@@ -316,8 +308,8 @@ void packed_attn_kernel(PackedArgs a) {
     }
 
     // A value that some row of the tile does not see may be infinite or NaN, and its weight 0 times that is NaN.
-    // Where that may have happened the item is done again, more slowly: such values are left out of PV, and a row
-    // gets their infinities and NaN where it has a weight on one, by a product of the weights with their places.
+    // Where that may have happened the item is done again, with the masked blocks' PV key by key for the rows that
+    // give the key a weight: slow, in few registers, and rare.
     if (n_full < n) {
       float zero = 0.f;
 #pragma unroll
@@ -333,38 +325,45 @@ void packed_attn_kernel(PackedArgs a) {
         for (int u = 0; u < 4; ++u)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[u][r] = 0.f;
+        // this wave's weights, [row][key]: the second buffers hold 8 KB for each of up to 4 waves
+        static_assert(NW <= 4, "room for the weights");
+        float* w_s = reinterpret_cast<float*>((wave & 2 ? v_s[1] : k_s[1]) + (wave & 1) * (kTileBytes / 2));
 #pragma unroll 1
         for (x = 0; x < n; ++x) {
-          const int par = x & 1;
-          load(true, x);
-          load(false, x);
+          __syncthreads();
+          load(true, x, 0);
+          load(false, x, 0);
           CHORUS_WAIT_LDS_TILES();
           __syncthreads();
-          vec8 pf[2][2];
-          qk(s0, k_s[par]);
+          qk(s0, k_s[0]);
           if (x >= n_full) mask(s0, limit(x));
           rescale(row_max(s0));
+          vec8 pf[2][2];
           probs(s0, pf);
           if (x < n_full) {
-            pv(pf, v_s[par]);
+            pv(pf, v_s[0]);
             continue;
           }
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) w_s[l32 * kBlock + 32 * t + 8 * (r >> 2) + 4 * hl + (r & 3)] = (float)pf[t][r >> 3][r & 7];
+          CHORUS_WAIT_LDS_TILES();
 #pragma unroll 1
-          for (int kind = -1; kind < 3; ++kind) {
-            const float what = kind < 1 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
-            int from = par * kTileBytes;
-            asm volatile("" : "+v"(from));   // read again each time: kept across the kinds the fragments would spill
+          for (int key = 0; key < kBlock; ++key) {
+            const float w = w_s[l32 * kBlock + key];
+            if (!(w == 0.f)) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              f32x16 hit;
+              for (int u = 0; u < 4; ++u)
 #pragma unroll
-              for (int r = 0; r < 16; ++r) hit[r] = kind < 0 ? o[u][r] : 0.f;
+                for (int rr = 0; rr < 4; ++rr) {
+                  const int d = 32 * u + 8 * rr + 4 * hl;
+                  const uint2 v4 = *reinterpret_cast<const uint2*>(v_s[0] + key * 256 + v_chunk(key, d >> 3) * 16 + (d & 4) * 2);
+                  scalar v[4];
+                  __builtin_memcpy(v, &v4, 8);
 #pragma unroll
-              for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) hit = T::mfma(pick<BF16>(fragment(v_s[0] + from, t, hh, u), kind), pf[t][hh], hit);
-#pragma unroll
-              for (int r = 0; r < 16; ++r) o[u][r] = kind < 0 ? hit[r] : hit[r] > 0.f ? o[u][r] + what : o[u][r];
+                  for (int e = 0; e < 4; ++e) o[u][4 * rr + e] += w * (float)v[e];
+                }
             }
           }
         }
@@ -373,22 +372,28 @@ void packed_attn_kernel(PackedArgs a) {
   }
 
   const float l_tot = pair_sum(l_run);
-  if (!valid) return;
+  // the row's place, worked out again: kept across the loops it would cost registers
+  int lane2 = tid & 63;
+  asm volatile("" : "+v"(lane2));
+  const int tile_row = wave * 32 + (lane2 & 31), hl2 = lane2 >> 5;
+  if (it.row0 + tile_row >= it.rows) return;
   if (it.slot >= 0) {
-    const int64_t at = ((int64_t)it.slot * a.Hk + hk) * (32 * NW) + wave * 32 + l32;
+    const int64_t at = ((int64_t)it.slot * a.Hk + hk) * (32 * NW) + tile_row;
     float* po = a.part_o + at * kHeadDim;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr)
-        *reinterpret_cast<float4*>(po + 32 * u + 8 * rr + 4 * hl) =
+        *reinterpret_cast<float4*>(po + 32 * u + 8 * rr + 4 * hl2) =
             make_float4(o[u][4 * rr], o[u][4 * rr + 1], o[u][4 * rr + 2], o[u][4 * rr + 3]);
-    if (hl == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m_run, l_tot);
+    if (hl2 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m_run, l_tot);
     return;
   }
+  const int token = in_group(a, it.row0 + tile_row);
+  const int64_t query = it.q0 + token, qh = hk * a.group + it.row0 + tile_row - token * a.group;
   const bool empty = l_tot == 0.f;   // NaN is not
   const float inv_l = empty ? 0.f : 1.f / l_tot;
-  uint16_t* op = static_cast<uint16_t*>(const_cast<void*>(a.o.data)) + (int64_t)(it.q0 + query) * a.o.ss + (int64_t)qh * a.o.sh;
+  uint16_t* op = static_cast<uint16_t*>(const_cast<void*>(a.o.data)) + query * a.o.ss + qh * a.o.sh;
 #pragma unroll
   for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -398,10 +403,10 @@ void packed_attn_kernel(PackedArgs a) {
       for (int e = 0; e < 4; ++e) v4[e] = (scalar)(o[u][4 * rr + e] * inv_l);
       uint2 packed;
       __builtin_memcpy(&packed, v4, 8);
-      *reinterpret_cast<uint2*>(op + 32 * u + 8 * rr + 4 * hl) = packed;
+      *reinterpret_cast<uint2*>(op + 32 * u + 8 * rr + 4 * hl2) = packed;
     }
-  if (a.lse && hl == 0)
-    a.lse[(int64_t)qh * a.total_q + it.q0 + query] = empty ? -INFINITY : (m_run + __builtin_log2f(l_tot)) * kLn2;
+  if (a.lse && hl2 == 0)
+    a.lse[qh * a.total_q + query] = empty ? -INFINITY : (m_run + __builtin_log2f(l_tot)) * kLn2;
 }
 
 // Joins a tile's pieces: with m the largest of their maxima, O = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.
@@ -463,7 +468,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
     for (int d = 16; d > 0; d >>= 1) l += __shfl_xor(l, d, 32);
     const bool empty = l == 0.f;
     const float inv_l = empty ? 0.f : 1.f / l;
-    const int query = jn.q0 + row / a.group, qh = hk * a.group + row % a.group;
+    const int token = in_group(a, row), query = jn.q0 + token, qh = hk * a.group + row - token * a.group;
     const scalar v4[4] = {(scalar)(o.x * inv_l), (scalar)(o.y * inv_l), (scalar)(o.z * inv_l), (scalar)(o.w * inv_l)};
     uint2 packed;
     __builtin_memcpy(&packed, v4, 8);
@@ -476,8 +481,11 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
 
 template <bool BF16, int NW>
 void launch_packed(const PackedConfig& c, const PackedArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((packed_attn_kernel<BF16, NW>), dim3((unsigned)packed_grid(a.Hk, c.max_items)), dim3(64 * NW), 0, st,
-                     a);
+  const dim3 grid = packed_grid(a.Hk, c.max_items), block(64 * NW);
+  if (a.prefix > 0)
+    hipLaunchKernelGGL((packed_attn_kernel<BF16, true, NW>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((packed_attn_kernel<BF16, false, NW>), grid, block, 0, st, a);
   const int64_t groups = (int64_t)c.max_joins * a.Hk * (32 * NW / 8);
   hipLaunchKernelGGL((packed_join_kernel<BF16, NW>), dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, a);
 }
