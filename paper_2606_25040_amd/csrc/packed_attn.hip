@@ -75,6 +75,20 @@ inline dim3 packed_grid(int Hk, int max_items) {
   return dim3(rounds ? kNumXcd * max_items : rest * max_items, rounds + (rest > 0));
 }
 
+// 16 bytes per lane from an address per lane to LDS (lane-linear at the wave-uniform byte address lds), as dma16.
+__device__ inline void dma16_from(uint32_t lds, const char* from) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(lds), "v"(from)
+      : "memory");
+}
+
 // row / group
 __device__ inline int in_group(const PackedArgs& a, int row) {
   return (int)(((uint64_t)(uint32_t)row * a.group_mul) >> a.group_shift);
@@ -155,28 +169,54 @@ void packed_attn_kernel(PackedArgs a) {
         dma16(lds + NW * u * 1024, from, (uint32_t)min(4 * NW * u + r0, rows - 1) * t.ss + c);
     }
   };
-  if (n > 0) load(true, 0, 0);
-
-  vec8 qf[8];
-  {
-    const int query = in_group(a, row), qh = hk * a.group + row - query * a.group;
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q.data) + (int64_t)(it.q0 + query) * a.q.ss +
-                         (int64_t)qh * a.q.sh + 8 * hl;
+  // Address of head dim 0 of tile row r (rows past the last: the last) in q or out.
+  auto row_at = [&](const TensorArg& t, int r) {
+    const int at = min(it.row0 + r, it.rows - 1), token = in_group(a, at);
+    return static_cast<char*>(const_cast<void*>(t.data)) + 2 * ((int64_t)(it.q0 + token) * t.ss + (int64_t)(hk * a.group + at - token * a.group) * t.sh);
+  };
+  // This wave's part of the second buffers: its Q rows at first, later its results.  Rows of 256 bytes, as K's.
+  char* mine_s = (wave & 2 ? v_s[1] : k_s[1]) + (wave & 1) * (kTileBytes / 2);
+  if (n > 0) {
+    load(true, 0, 0);
+    const uint32_t lds = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)mine_s;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      if (valid) {
-        qf[s] = *reinterpret_cast<const vec8*>(qp + 16 * s);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qf[s][e] = (scalar)0.f;
-      }
+    for (int u = 0; u < 8; ++u) {
+      const int r = 4 * u + (lane >> 4);
+      dma16_from(lds + u * 1024, row_at(a.q, wave * 32 + r) + 16 * k_chunk(r, lane & 15));
     }
+    load(false, 0, 0);
+    if (tid == 0) again = 0;
+    CHORUS_WAIT_VMCNT(4);   // all but V's
   }
-  __builtin_amdgcn_sched_barrier(0);   // the loads that may still be on their way come after Q's
-  if (n > 0) load(false, 0, 0);
-  if (n > 1) load(true, 1, 1);
   const int k_row_off = l32 * 256;
   const int k_sw = l32 & 15;
+  vec8 qf[8];
+#pragma unroll
+  for (int d = 0; d < 8; ++d) qf[d] = *reinterpret_cast<const vec8*>(mine_s + k_row_off + (((2 * d + hl) ^ k_sw) << 4));
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // Q is read before its place is filled
+  __syncthreads();
+  if (n > 1) load(true, 1, 1);
+  if (it.row0 + wave * 32 >= it.rows) {
+    // a wave without rows only loads its share
+    for (int x = 0; x < n; ++x) {
+      CHORUS_WAIT_LDS_TILES();
+      __syncthreads();
+      if (x + 2 < n) load(true, x + 2, x & 1);
+      if (x + 1 < n) load(false, x + 1, (x + 1) & 1);
+    }
+    if (n_full < n) {
+      __syncthreads();
+      for (int x = 0; again && x < n; ++x) {
+        __syncthreads();
+        load(true, x, 0);
+        load(false, x, 0);
+        CHORUS_WAIT_LDS_TILES();
+        __syncthreads();
+      }
+    }
+    __syncthreads();
+    return;
+  }
   const int v_lane_off = (j16 >> 2) * 256 + 8 * (j16 & 1) + 4 * (g >> 1) * 256;
   const int v_c0 = 2 * (g & 1) + ((j16 & 3) >> 1);
   const int v_sw = v_bits(j16 >> 2);
@@ -262,13 +302,6 @@ void packed_attn_kernel(PackedArgs a) {
   if (n > 0) {
     f32x16 s0[2], s1[2];
     float mx;
-    if (tid == 0) again = 0;
-    // Q and the first K tile have landed; the next K and the first V tile may be on their way
-    if (n > 1)
-      CHORUS_WAIT_VMCNT(8);
-    else
-      CHORUS_WAIT_VMCNT(4);
-    __syncthreads();
     qk(s0, k_s[0]);
     if (n_full == 0) mask(s0, limit(0));
     mx = row_max(s0);
@@ -327,7 +360,7 @@ void packed_attn_kernel(PackedArgs a) {
           for (int r = 0; r < 16; ++r) o[u][r] = 0.f;
         // this wave's weights, [row][key]: the second buffers hold 8 KB for each of up to 4 waves
         static_assert(NW <= 4, "room for the weights");
-        float* w_s = reinterpret_cast<float*>((wave & 2 ? v_s[1] : k_s[1]) + (wave & 1) * (kTileBytes / 2));
+        float* w_s = reinterpret_cast<float*>(mine_s);
 #pragma unroll 1
         for (x = 0; x < n; ++x) {
           __syncthreads();
@@ -372,28 +405,39 @@ void packed_attn_kernel(PackedArgs a) {
   }
 
   const float l_tot = pair_sum(l_run);
-  // the row's place, worked out again: kept across the loops it would cost registers
-  int lane2 = tid & 63;
-  asm volatile("" : "+v"(lane2));
-  const int tile_row = wave * 32 + (lane2 & 31), hl2 = lane2 >> 5;
-  if (it.row0 + tile_row >= it.rows) return;
-  if (it.slot >= 0) {
-    const int64_t at = ((int64_t)it.slot * a.Hk + hk) * (32 * NW) + tile_row;
-    float* po = a.part_o + at * kHeadDim;
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int rr = 0; rr < 4; ++rr)
-        *reinterpret_cast<float4*>(po + 32 * u + 8 * rr + 4 * hl2) =
-            make_float4(o[u][4 * rr], o[u][4 * rr + 1], o[u][4 * rr + 2], o[u][4 * rr + 3]);
-    if (hl2 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m_run, l_tot);
-    return;
-  }
-  const int token = in_group(a, it.row0 + tile_row);
-  const int64_t query = it.q0 + token, qh = hk * a.group + it.row0 + tile_row - token * a.group;
   const bool empty = l_tot == 0.f;   // NaN is not
   const float inv_l = empty ? 0.f : 1.f / l_tot;
-  uint16_t* op = static_cast<uint16_t*>(const_cast<void*>(a.o.data)) + query * a.o.ss + qh * a.o.sh;
+  CHORUS_WAIT_LDS_TILES();
+  __syncthreads();                   // the tiles are done with
+  // the rows' places, worked out again: kept across the loops they would cost registers
+  int lane2 = tid & 63;
+  asm volatile("" : "+v"(lane2));
+  const int r32 = lane2 & 31, hl2 = lane2 >> 5;
+  const int left = it.rows - it.row0 - wave * 32;   // rows of this wave
+  // Results go through LDS, so that each store writes whole rows: written from the accumulators, 16 bytes of each
+  // of 32 rows at a time, 25,600 x 24 rows without keys took 98 us.
+  if (it.slot >= 0) {
+    const int64_t at = ((int64_t)it.slot * a.Hk + hk) * (32 * NW) + wave * 32;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {   // 64 of a row's 128 values fit the wave's 8 KB
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) {
+          const f32x16& v = o[2 * half + u];
+          *reinterpret_cast<float4*>(mine_s + r32 * 256 + k_chunk(r32, 8 * u + 2 * rr + hl2) * 16) =
+              make_float4(v[4 * rr], v[4 * rr + 1], v[4 * rr + 2], v[4 * rr + 3]);
+        }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int r = 4 * u + (lane2 >> 4), c = lane2 & 15;
+        const float4 v = *reinterpret_cast<const float4*>(mine_s + r * 256 + k_chunk(r, c) * 16);
+        if (r < left) *reinterpret_cast<float4*>(a.part_o + (at + r) * kHeadDim + 64 * half + 4 * c) = v;
+      }
+    }
+    if (hl2 == 0 && r32 < left) *reinterpret_cast<float2*>(a.part_ml + 2 * (at + r32)) = make_float2(m_run, l_tot);
+    return;
+  }
 #pragma unroll
   for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -403,10 +447,19 @@ void packed_attn_kernel(PackedArgs a) {
       for (int e = 0; e < 4; ++e) v4[e] = (scalar)(o[u][4 * rr + e] * inv_l);
       uint2 packed;
       __builtin_memcpy(&packed, v4, 8);
-      *reinterpret_cast<uint2*>(op + 32 * u + 8 * rr + 4 * hl2) = packed;
+      *reinterpret_cast<uint2*>(mine_s + r32 * 256 + k_chunk(r32, 4 * u + rr) * 16 + 8 * hl2) = packed;
     }
-  if (a.lse && hl2 == 0)
-    a.lse[qh * a.total_q + query] = empty ? -INFINITY : (m_run + __builtin_log2f(l_tot)) * kLn2;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const int r = 4 * u + (lane2 >> 4), c = lane2 & 15;
+    const uint4 v = *reinterpret_cast<const uint4*>(mine_s + r * 256 + k_chunk(r, c) * 16);
+    if (r < left) *reinterpret_cast<uint4*>(row_at(a.o, wave * 32 + r) + 16 * c) = v;
+  }
+  if (a.lse && hl2 == 0 && r32 < left) {
+    const int row = it.row0 + wave * 32 + r32, token = in_group(a, row);
+    a.lse[(int64_t)(hk * a.group + row - token * a.group) * a.total_q + it.q0 + token] =
+        empty ? -INFINITY : (m_run + __builtin_log2f(l_tot)) * kLn2;
+  }
 }
 
 // Joins a tile's pieces: with m the largest of their maxima, O = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.
