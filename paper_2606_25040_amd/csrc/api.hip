@@ -813,7 +813,7 @@ chorus_status chorus_plan_packed_attn(const chorus_packed_shape* shape, const in
 // Unfinished results: per slot, key head and row of a tile 128 values of O, the running maximum and the sum.
 static void carve_parts(void* ws, const chorus_packed_shape& s, const PackedConfig& c, float** o, float** ml, size_t* bytes) {
   Carver v(ws);
-  const size_t rows = (size_t)c.max_slots * s.kv_heads * 32 * c.waves;
+  const size_t rows = (size_t)c.max_slots * s.kv_heads * kPackedTile;
   *o = v.take<float>(rows * kHeadDim);
   *ml = v.take<float>(rows * 2);
   *bytes = align_up(v.used, 256);

@@ -147,8 +147,8 @@ hipError_t launch_qk_norm_rope(chorus_dtype dt, RopeArgs a, hipStream_t st);
 // ---- attention over packed sequences (packed_plan.hip, packed_attn.hip) ----
 // How a shape is cut, from host-known sizes only; the same for the plan and
 // the attention that runs it.
+constexpr int kPackedWaves = 4, kPackedTile = 32 * kPackedWaves;   // query rows of a tile, 32 per wave
 struct PackedConfig {
-  int waves;           // of 32 query rows: a tile has 32 * waves rows
   int pooled;          // the prefix is a pass of its own over the rows of all sequences
   int per_head;        // pieces of one key head that fill the GPU
   int32_t max_items, max_slots, max_joins;   // what a plan can come to

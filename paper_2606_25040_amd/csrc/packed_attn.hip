@@ -21,6 +21,9 @@ namespace {
 constexpr float kRescaleLog2 = 8.f;
 constexpr int kTileBytes = kBlock * kHeadDim * 2;
 
+// This wave's LDS reads have returned and its LDS writes are done.
+#define CHORUS_WAIT_LDS() asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory")
+
 // 16-byte chunk of row r that holds chunk c: the b128 reads of K and the transposed b64 reads of V then spread over
 // all LDS banks.
 __device__ inline int k_chunk(int r, int c) { return c ^ (r & 15); }
@@ -103,12 +106,13 @@ struct Rows {
   __device__ const char* at(int block) const { return base + (int64_t)block * kBlock * ss; }
 };
 
-template <bool BF16, bool PREFIX, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
+template <bool BF16, bool CAUSAL, bool PREFIX>
+__global__ __launch_bounds__(64 * kPackedWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void packed_attn_kernel(PackedArgs a) {
   using T = Type<BF16>;
   using vec8 = typename T::vec8;
   using scalar = typename T::scalar;
+  constexpr int NW = kPackedWaves, kTile = kPackedTile;
   __shared__ __attribute__((aligned(1024))) char k_s[2][kTileBytes];
   __shared__ __attribute__((aligned(1024))) char v_s[2][kTileBytes];
   __shared__ int again;
@@ -131,9 +135,9 @@ void packed_attn_kernel(PackedArgs a) {
   const bool valid = row < it.rows;
   // own keys that a row sees: this lane's, and the fewest and most of the tile
   const int shift = it.nk - nq + 1;
-  auto sees = [&](int r) { return a.causal ? min(max(in_group(a, r) + shift, 0), it.nk) : it.nk; };
+  auto sees = [&](int r) { return CAUSAL ? min(max(in_group(a, r) + shift, 0), it.nk) : it.nk; };
   const int seen = valid ? sees(row) : 0;
-  const int seen_first = sees(it.row0), seen_last = sees(min(it.row0 + 32 * NW, it.rows) - 1);
+  const int seen_first = sees(it.row0), seen_last = sees(min(it.row0 + kTile, it.rows) - 1);
   const int prefix = !PREFIX || (a.pooled && it.k0 >= 0) ? 0 : a.prefix;
   const int pw = prefix / kBlock;                                     // whole prefix blocks
   const int own = (seen_last + kBlock - 1) / kBlock;
@@ -169,6 +173,20 @@ void packed_attn_kernel(PackedArgs a) {
         dma16(lds + NW * u * 1024, from, (uint32_t)min(4 * NW * u + r0, rows - 1) * t.ss + c);
     }
   };
+  // V rows past the block's end: zeros, by the wave that loaded them, before the barrier that publishes them (a weight
+  // of 0 on an infinite value would be NaN).
+  auto trim = [&](int x) {
+    const int j = it.j0 + x;
+    const bool mine = !PREFIX || (j >= pw && j < pw + own);
+    const int rows = (mine ? it.nk : prefix) - (mine ? j - pw : min(j, pw)) * kBlock;
+    if (rows >= kBlock) return;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));   // worked out here: kept across the loops the addresses would cost registers
+#pragma unroll
+    for (int u = 0; u < 16 / NW; ++u)
+      if (4 * (NW * u + wave) + (ln >> 4) >= rows)
+        *reinterpret_cast<uint4*>(v_s[x & 1] + (NW * u + wave) * 1024 + ln * 16) = make_uint4(0, 0, 0, 0);
+  };
   // Address of head dim 0 of tile row r (rows past the last: the last) in q or out.
   auto row_at = [&](const TensorArg& t, int r) {
     const int at = min(it.row0 + r, it.rows - 1), token = in_group(a, at);
@@ -185,7 +203,7 @@ void packed_attn_kernel(PackedArgs a) {
       dma16_from(lds + u * 1024, row_at(a.q, wave * 32 + r) + 16 * k_chunk(r, lane & 15));
     }
     load(false, 0, 0);
-    if (tid == 0) again = 0;
+    if (CAUSAL && tid == 0) again = 0;
     CHORUS_WAIT_VMCNT(4);   // all but V's
   }
   const int k_row_off = l32 * 256;
@@ -193,18 +211,20 @@ void packed_attn_kernel(PackedArgs a) {
   vec8 qf[8];
 #pragma unroll
   for (int d = 0; d < 8; ++d) qf[d] = *reinterpret_cast<const vec8*>(mine_s + k_row_off + (((2 * d + hl) ^ k_sw) << 4));
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // Q is read before its place is filled
+  CHORUS_WAIT_LDS();   // Q is read before its place is filled
   __syncthreads();
   if (n > 1) load(true, 1, 1);
   if (it.row0 + wave * 32 >= it.rows) {
     // a wave without rows only loads its share
     for (int x = 0; x < n; ++x) {
       CHORUS_WAIT_LDS_TILES();
+      if (x >= n_full) trim(x);
+      CHORUS_WAIT_LDS();
       __syncthreads();
       if (x + 2 < n) load(true, x + 2, x & 1);
       if (x + 1 < n) load(false, x + 1, (x + 1) & 1);
     }
-    if (n_full < n) {
+    if (CAUSAL && n_full < n && seen_first < seen_last) {
       __syncthreads();
       for (int x = 0; again && x < n; ++x) {
         __syncthreads();
@@ -323,9 +343,12 @@ void packed_attn_kernel(PackedArgs a) {
       fused(x, 0, s0, s1);
       fused(x + 1, 1, s1, s0);
     }
+    // the blocks that need a mask, and up to two ahead of them
     for (; x < n; ++x) {
       const int par = x & 1;
       CHORUS_WAIT_LDS_TILES();
+      if (x >= n_full) trim(x);
+      CHORUS_WAIT_LDS();
       __syncthreads();
       if (x + 2 < n) load(true, x + 2, x & 1);
       if (x + 1 < n) load(false, x + 1, (x + 1) & 1);
@@ -340,10 +363,10 @@ void packed_attn_kernel(PackedArgs a) {
       }
     }
 
-    // A value that some row of the tile does not see may be infinite or NaN, and its weight 0 times that is NaN.
+    // A value that some row of the tile sees and another does not may be infinite or NaN, and a weight of 0 on it NaN.
     // Where that may have happened the item is done again, with the masked blocks' PV key by key for the rows that
     // give the key a weight: slow, in few registers, and rare.
-    if (n_full < n) {
+    if (CAUSAL && n_full < n && seen_first < seen_last) {
       float zero = 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u)
@@ -359,7 +382,6 @@ void packed_attn_kernel(PackedArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[u][r] = 0.f;
         // this wave's weights, [row][key]: the second buffers hold 8 KB for each of up to 4 waves
-        static_assert(NW <= 4, "room for the weights");
         float* w_s = reinterpret_cast<float*>(mine_s);
 #pragma unroll 1
         for (x = 0; x < n; ++x) {
@@ -367,7 +389,7 @@ void packed_attn_kernel(PackedArgs a) {
           load(true, x, 0);
           load(false, x, 0);
           CHORUS_WAIT_LDS_TILES();
-          __syncthreads();
+          __syncthreads();   // (rows past the end have weight 0 and are passed over)
           qk(s0, k_s[0]);
           if (x >= n_full) mask(s0, limit(x));
           rescale(row_max(s0));
@@ -417,7 +439,7 @@ void packed_attn_kernel(PackedArgs a) {
   // Results go through LDS, so that each store writes whole rows: written from the accumulators, 16 bytes of each
   // of 32 rows at a time, 25,600 x 24 rows without keys took 98 us.
   if (it.slot >= 0) {
-    const int64_t at = ((int64_t)it.slot * a.Hk + hk) * (32 * NW) + wave * 32;
+    const int64_t at = ((int64_t)it.slot * a.Hk + hk) * kTile + wave * 32;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {   // 64 of a row's 128 values fit the wave's 8 KB
 #pragma unroll
@@ -464,10 +486,10 @@ void packed_attn_kernel(PackedArgs a) {
 
 // Joins a tile's pieces: with m the largest of their maxima, O = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.
 // 32 lanes per row, a workgroup for 8 rows at a time; the maxima of up to 32 pieces are read at once.
-template <bool BF16, int NW>
+template <bool BF16>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   using scalar = typename Type<BF16>::scalar;
-  constexpr int kTile = 32 * NW, kGroups = kTile / 8;
+  constexpr int kTile = kPackedTile, kGroups = kTile / 8;
   const int* header = a.plan.header;
   if (header[kPlanKey] != a.key) return;
   const int np = header[kPlanPrefixPieces], first_row = header[kPlanFirstRow];
@@ -532,24 +554,28 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   }
 }
 
-template <bool BF16, int NW>
+template <bool BF16>
 void launch_packed(const PackedConfig& c, const PackedArgs& a, hipStream_t st) {
-  const dim3 grid = packed_grid(a.Hk, c.max_items), block(64 * NW);
-  if (a.prefix > 0)
-    hipLaunchKernelGGL((packed_attn_kernel<BF16, true, NW>), grid, block, 0, st, a);
+  const dim3 grid = packed_grid(a.Hk, c.max_items), block(64 * kPackedWaves);
+  if (a.causal && a.prefix > 0)
+    hipLaunchKernelGGL((packed_attn_kernel<BF16, true, true>), grid, block, 0, st, a);
+  else if (a.causal)
+    hipLaunchKernelGGL((packed_attn_kernel<BF16, true, false>), grid, block, 0, st, a);
+  else if (a.prefix > 0)
+    hipLaunchKernelGGL((packed_attn_kernel<BF16, false, true>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((packed_attn_kernel<BF16, false, NW>), grid, block, 0, st, a);
-  const int64_t groups = (int64_t)c.max_joins * a.Hk * (32 * NW / 8);
-  hipLaunchKernelGGL((packed_join_kernel<BF16, NW>), dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((packed_attn_kernel<BF16, false, false>), grid, block, 0, st, a);
+  const int64_t groups = (int64_t)c.max_joins * a.Hk * (kPackedTile / 8);
+  hipLaunchKernelGGL((packed_join_kernel<BF16>), dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, a);
 }
 
 }  // namespace
 
 hipError_t launch_packed_attn(chorus_dtype dt, const PackedConfig& c, const PackedArgs& a, hipStream_t st) {
   if (dt == CHORUS_BF16)
-    launch_packed<true, 4>(c, a, st);
+    launch_packed<true>(c, a, st);
   else
-    launch_packed<false, 4>(c, a, st);
+    launch_packed<false>(c, a, st);
   return hipGetLastError();
 }
 

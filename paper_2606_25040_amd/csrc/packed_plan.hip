@@ -1,7 +1,7 @@
 // Work plan of attention over packed sequences: from the lengths on the device to a list of workgroups.
 //
 // Every sequence's query rows (query * group + head in group, so that the heads that share a key head share its
-// tiles) are cut into tiles of 32 * waves rows, and a tile's key blocks (64 keys) into pieces where whole tiles
+// tiles) are cut into tiles of kPackedTile rows, and a tile's key blocks (64 keys) into pieces where whole tiles
 // would leave the GPU unevenly filled: with C key blocks in all, a piece has about C / per_head blocks.  A prefix
 // is either part of each tile's key blocks, or, pooled, a pass of its own whose tiles run over the rows of all
 // sequences, so its keys are read once per tile of rows and not once per sequence.  Items are listed longest
@@ -34,8 +34,7 @@ PackedConfig packed_config(const chorus_packed_shape& s) {
   PackedConfig c;
   const int group = s.q_heads / s.kv_heads;
   const int64_t rows = (int64_t)s.total_q * group;
-  c.waves = 4;
-  const int tile = 32 * c.waves;
+  const int tile = kPackedTile;
   // The prefix is worth a pass of its own when the sequences' own tiles are mostly empty: then a tile of pooled
   // rows replaces several walks over it.
   c.pooled = s.prefix > 0 && s.n_seqs > 1 && rows < (int64_t)s.n_seqs * tile;
@@ -53,7 +52,7 @@ PackedConfig packed_config(const chorus_packed_shape& s) {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kMaxThreads = 1024;
 
 struct PlanArgs {
   const int32_t* q_offsets;
@@ -65,19 +64,19 @@ struct PlanArgs {
 };
 
 // Inclusive scan over the workgroup (every thread takes part); `total` is the last thread's value.
-template <class Op>
-__device__ inline int block_scan(int v, Op op, int* wave_s, int* total) {
+template <class T, class Op>
+__device__ inline T block_scan(T v, Op op, T* wave_s, T* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int u = __shfl_up(v, d);
+    const T u = __shfl_up(v, d);
     if (lane >= d) v = op(u, v);
   }
   __syncthreads();
   if (lane == 63) wave_s[wave] = v;
   __syncthreads();
-  int before = 0;
-  for (int w = 0; w < kThreads / 64; ++w) {
+  T before = 0;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
     if (w == wave && w > 0) v = op(before, v);
     before = w ? op(before, wave_s[w]) : wave_s[0];
   }
@@ -86,7 +85,8 @@ __device__ inline int block_scan(int v, Op op, int* wave_s, int* total) {
 }
 
 struct Add {
-  __device__ int operator()(int a, int b) const { return a + b; }
+  template <class T>
+  __device__ T operator()(T a, T b) const { return a + b; }
 };
 struct Max {
   __device__ int operator()(int a, int b) const { return a > b ? a : b; }
@@ -125,9 +125,9 @@ __device__ inline Tile tile_at(const PlanArgs& a, const Seqs& seqs, int t) {
 }
 
 template <bool NEAR>
-__global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
-  __shared__ int wave_s[kThreads / 64];
-  __shared__ unsigned long long cost_s;
+__global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
+  __shared__ int wave_s[kMaxThreads / 64];
+  __shared__ unsigned long long cost_s, wave_l[kMaxThreads / 64];
   __shared__ int flags_s, class_s[kClasses];
   __shared__ PackedSeq near_s[NEAR ? kNear + 1 : 1];
   PackedSeq* far = a.plan.seqs;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
       return far;
   };
   auto& seq = seqs();
-  const int tid = threadIdx.x, N = a.n_seqs;
+  const int tid = threadIdx.x, threads = blockDim.x, N = a.n_seqs;
   if (tid == 0) {
     cost_s = 0;
     flags_s = 0;
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   if (tid < kClasses) class_s[tid] = 0;
   // key rows first: their loads are in flight during the first scan
   int flags = 0;
-  for (int i = tid; i < N; i += kThreads) {
+  for (int i = tid; i < N; i += threads) {
     const int raw0 = a.k_offsets[i];
     const int64_t raw = a.k_lens ? a.k_lens[i] : (int64_t)a.k_offsets[i + 1] - raw0;
     const int k0 = min(max(raw0, 0), a.total_k);
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
     seq[i].nk = nk;
   }
   int run = 0, total;
-  for (int base = 0; base <= N; base += kThreads) {
+  for (int base = 0; base <= N; base += threads) {
     const int i = base + tid;
     const int raw = i <= N ? a.q_offsets[i] : 0;
     const int v = max(run, block_scan(min(max(raw, 0), a.total_q), Max(), wave_s, &total));
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   if (flags) atomicOr(&flags_s, flags);
   __syncthreads();
   run = 0;
-  for (int base = 0; base < N; base += kThreads) {
+  for (int base = 0; base < N; base += threads) {
     const int i = base + tid;
     int tiles = 0;
     if (i < N) {
@@ -190,20 +190,24 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   // this thread's first tile is kept; most plans have no second
   const Tile mine = tid < n_tiles ? tile_at(a, seq, tid) : Tile{};
   unsigned long long cost = mine.blocks;
-  for (int t = tid + kThreads; t < n_tiles; t += kThreads) cost += tile_at(a, seq, t).blocks;
+  for (int t = tid + threads; t < n_tiles; t += threads) cost += tile_at(a, seq, t).blocks;
   if (cost) atomicAdd(&cost_s, cost);
   __syncthreads();
   cost = cost_s + (unsigned long long)pooled_tiles * prefix_blocks;
-  const int piece = max((int)min((cost + a.per_head - 1) / a.per_head, 1ull << 26), kMinChunk);
+  // (the quotient in fp32: which blocks make a piece may be off by one in 2^24)
+  const int piece = max((int)min((float)cost / (float)a.per_head + 1.f, (float)(1 << 26)), kMinChunk);
   const int longest = piece + piece / 2;
   auto pieces = [&](int blocks) { return blocks > longest ? (blocks + piece - 1) / piece : 1; };
+  const float per_class = (float)kClasses / (float)(longest + 1);
+  // first block of piece i of p
+  auto cut = [](int blocks, int p, int i) { return blocks / p * i + min(blocks % p, i); };
   auto class_of = [&](int blocks, int p) {
-    return kClasses - 1 - (int)((int64_t)((blocks + p - 1) / p) * kClasses / (longest + 1));
+    return kClasses - 1 - min((int)((float)((blocks + p - 1) / p) * per_class), kClasses - 1);
   };
   const int np = pooled_tiles ? pieces(prefix_blocks) : 0;
 
-  for (int t = tid; t < n_tiles; t += kThreads) {
-    const int n = t < kThreads ? mine.blocks : tile_at(a, seq, t).blocks, p = pieces(n);
+  for (int t = tid; t < n_tiles; t += threads) {
+    const int n = t < threads ? mine.blocks : tile_at(a, seq, t).blocks, p = pieces(n);
     if (n > 0 || !a.pooled) atomicAdd(&class_s[class_of(n, p)], p);
   }
   if (tid == 0 && np) atomicAdd(&class_s[class_of(prefix_blocks, np)], pooled_tiles * np);
@@ -221,14 +225,14 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   }
   __syncthreads();
 
-  for (int x = tid; x < pooled_tiles * np; x += kThreads) {
+  for (int x = tid; x < pooled_tiles * np; x += threads) {
     const int t = x / np, i = x % np;
     const int at = atomicAdd(&class_s[class_of(prefix_blocks, np)], 1);
-    a.plan.items[at] = {first, t * a.tile, pooled_rows, (int)((int64_t)i * prefix_blocks / np),
-                        (int)((int64_t)(i + 1) * prefix_blocks / np), -1, 0, x};
+    a.plan.items[at] = {first, t * a.tile, pooled_rows, cut(prefix_blocks, np, i),
+                        cut(prefix_blocks, np, i + 1), -1, 0, x};
   }
   int slots = pooled_tiles * np, joins = 0;
-  for (int base = 0; base < n_tiles; base += kThreads) {
+  for (int base = 0; base < n_tiles; base += threads) {
     const int t = base + tid;
     Tile x = {};
     int p = 0, own = 0, joined = 0;
@@ -238,16 +242,16 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
       joined = a.pooled || p > 1;
       own = joined ? p : 0;
     }
-    int slot_total, join_total;
-    const int slot = slots + block_scan(own, Add(), wave_s, &slot_total) - own;
-    const int join = joins + block_scan(joined, Add(), wave_s, &join_total) - joined;
-    slots += slot_total;
-    joins += join_total;
+    unsigned long long both = (unsigned long long)own << 32 | joined, upto;   // slots and joins in one scan
+    both = block_scan(both, Add(), wave_l, &upto) - both;
+    const int slot = slots + (int)(both >> 32), join = joins + (int)(uint32_t)both;
+    slots += (int)(upto >> 32);
+    joins += (int)(uint32_t)upto;
     if (p) {
       int at = atomicAdd(&class_s[class_of(x.blocks, p)], p);
       for (int i = 0; i < p; ++i, ++at)
-        a.plan.items[at] = {x.seq.q0, x.row0, x.rows, (int)((int64_t)i * x.blocks / p),
-                            (int)((int64_t)(i + 1) * x.blocks / p), x.seq.k0, x.seq.nk, joined ? slot + i : -1};
+        a.plan.items[at] = {x.seq.q0, x.row0, x.rows, cut(x.blocks, p, i), cut(x.blocks, p, i + 1),
+                            x.seq.k0, x.seq.nk, joined ? slot + i : -1};
     }
     if (joined) a.plan.joins[join] = {x.seq.q0, x.row0, x.rows, slot, p, {0, 0, 0}};
   }
@@ -265,11 +269,14 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
 hipError_t launch_packed_plan(const chorus_packed_shape& s, const PackedConfig& c, const int32_t* q_offsets,
                               const int32_t* k_offsets, const int32_t* k_lens, const PackedPlan& plan, hipStream_t st) {
   const PlanArgs a = {q_offsets, k_offsets, k_lens,   plan,       s.n_seqs, s.total_q,  s.total_k, s.prefix,
-                      s.q_heads / s.kv_heads, s.causal, 32 * c.waves, c.pooled, c.per_head, c.key};
+                      s.q_heads / s.kv_heads, s.causal, kPackedTile, c.pooled, c.per_head, c.key};
+  // a thread for each sequence and tile, as far as a workgroup goes: few threads pass its barriers sooner
+  const int most = std::max(s.n_seqs + 1, std::min(c.max_items, kMaxThreads));
+  const int threads = std::min((most + 63) / 64 * 64, kMaxThreads);
   if (s.n_seqs <= kNear)
-    hipLaunchKernelGGL((packed_plan_kernel<true>), dim3(1), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((packed_plan_kernel<true>), dim3(1), dim3(threads), 0, st, a);
   else
-    hipLaunchKernelGGL((packed_plan_kernel<false>), dim3(1), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((packed_plan_kernel<false>), dim3(1), dim3(threads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -238,6 +238,17 @@ def test_values_that_are_not_finite_reach_the_rows_that_see_them(dtype):
     near(got, clean, W, list(range(100)))
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_infinite_values_at_the_end_of_a_partial_block(dtype):
+    """Seen by every row: infinite in every row, and not NaN from the rows of the tile behind them."""
+    b = Batch([40, 9, 1], [70, 3, 500], 2, 1, dtype, causal=False, prefix=33)
+    b.v[69, 0, 5], b.v[72, 0, 90], b.pv[32, 0, 7] = float("inf"), float("-inf"), float("inf")
+    out = b.run()[0]
+    assert torch.isposinf(out[:40, :, 5]).all() and torch.isneginf(out[40:49, :, 90]).all() and torch.isposinf(out[:, :, 7]).all()
+    out[:40, :, 5], out[40:49, :, 90], out[:, :, 7] = 0, 0, 0
+    assert torch.isfinite(out).all()
+
+
 def test_logits_of_minus_infinity():
     """Keys whose logit is -inf carry no weight, also where a whole block or a row has nothing else."""
     b = Batch([1, 1, 2], [200, 64, 70], 2, 1, BF16)
