@@ -558,7 +558,8 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
  * call runs it, for every layer of the step alike.
  *
  * shape     : host struct.  max_q is a bound on the queries of one sequence (0:
- *             unknown); it only picks tile sizes, longer sequences stay right.
+ *             unknown); it only picks how the work is cut, longer sequences stay
+ *             right.
  * q_offsets : device int32 [n_seqs + 1], non-decreasing, within [0, total_q].
  * k_offsets : device int32 [n_seqs + 1] ([n_seqs] are read with k_lens, in any
  *             order, overlaps allowed), within [0, total_k].
@@ -579,8 +580,9 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
  * Results are bitwise deterministic for given lengths and inputs.  A row's
  * rounding may depend on the other sequences of the batch (how many pieces its
  * keys are cut into), as in chorus_block_sparse_attn_fwd.
- * Supports q_heads a multiple of kv_heads, total_q * q_heads < 2^31 and up to
- * 2^20 sequences.
+ * Supports q_heads a multiple of kv_heads, total_q * q_heads < 2^31, about 8
+ * million tiles (total_q * q_heads / kv_heads / 128 + n_seqs, over the smaller
+ * of kv_heads and 8) and up to 2^20 sequences.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t n_seqs;    /* >= 1                                       */

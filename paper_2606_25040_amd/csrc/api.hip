@@ -773,8 +773,9 @@ static chorus_status check_packed_shape(const chorus_packed_shape* s) {
   if (s->D != kHeadDim) return fail(CHORUS_ERR_UNSUPPORTED, "head dim D=%d unsupported (only 128)", s->D);
   if (s->causal != 0 && s->causal != 1) return fail(CHORUS_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (s->n_seqs > (1 << 20)) return fail(CHORUS_ERR_UNSUPPORTED, "more than 2^20 sequences");
+  // a launch holds less than 2^32 threads in one dimension, and 65,535 blocks in the other
   if ((int64_t)s->total_q * s->q_heads > INT32_MAX || s->kv_heads > 65535 ||
-      (int64_t)packed_config(*s).max_items * s->kv_heads > INT32_MAX / 2)
+      packed_config(*s).max_items * std::min(s->kv_heads, kNumXcd) * 64 * kPackedWaves > INT32_MAX)
     return fail(CHORUS_ERR_UNSUPPORTED, "too many query rows");
   return CHORUS_OK;
 }
@@ -813,7 +814,7 @@ chorus_status chorus_plan_packed_attn(const chorus_packed_shape* shape, const in
 // Unfinished results: per slot, key head and row of a tile 128 values of O, the running maximum and the sum.
 static void carve_parts(void* ws, const chorus_packed_shape& s, const PackedConfig& c, float** o, float** ml, size_t* bytes) {
   Carver v(ws);
-  const size_t rows = (size_t)c.max_slots * s.kv_heads * kPackedTile;
+  const size_t rows = ((size_t)c.max_slots * kPackedTile + c.row_slots) * s.kv_heads;
   *o = v.take<float>(rows * kHeadDim);
   *ml = v.take<float>(rows * 2);
   *bytes = align_up(v.used, 256);
@@ -883,7 +884,8 @@ chorus_status chorus_packed_attn_fwd(chorus_dtype dtype, const chorus_packed_sha
   a.group_mul = (uint32_t)(((1ull << (31 + l)) + a.group - 1) / a.group);
   a.causal = shape->causal;
   a.pooled = c.pooled;
-  a.max_items = c.max_items;
+  a.max_items = (int)c.max_items;
+  a.by_row = c.max_slots * kPackedTile * shape->kv_heads;
   a.key = c.key;
   a.sm_scale = sm_scale;
   return from_hip(launch_packed_attn(dtype, c, a, static_cast<hipStream_t>(stream)), "packed_attn");

@@ -151,7 +151,8 @@ constexpr int kPackedWaves = 4, kPackedTile = 32 * kPackedWaves;   // query rows
 struct PackedConfig {
   int pooled;          // the prefix is a pass of its own over the rows of all sequences
   int per_head;        // pieces of one key head that fill the GPU
-  int32_t max_items, max_slots, max_joins;   // what a plan can come to
+  int64_t max_items, max_slots, max_joins;   // what a plan can come to
+  int64_t row_slots;   // rows of all sequences whose results are kept by row
   int32_t key;         // of the shape, in the plan's header
 };
 PackedConfig packed_config(const chorus_packed_shape& s);
@@ -165,13 +166,15 @@ struct PackedSeq {     // rows of q from q0 (to the next one's), first tile, key
 // One workgroup's work for one key head: the query rows [row0, row0 + tile) of
 // the sequence that starts at query q0 and has `rows` of them (row = query *
 // group + head in group), over its key blocks [j0, j1).  k0 = -1: rows of all
-// sequences against the prefix.  slot: where the unfinished result goes, -1:
-// it is finished and goes to out.
+// sequences against the prefix.  slot: where an unfinished result goes, or one
+// of the two below.
+constexpr int kFinished = -1;   // to out
+constexpr int kByRow = -2;      // unfinished, by row of all sequences
 struct PackedItem {
   int32_t q0, row0, rows, j0, j1, k0, nk, slot;
 };
 // Rows [row0, row0 + tile) of a sequence whose result is in the slots slot ..
-// slot + pieces - 1, and in the prefix' slots.
+// slot + pieces - 1 (or kByRow), and in the prefix' slots.
 struct PackedJoin {
   int32_t q0, row0, rows, slot, pieces, unused[3];
 };
@@ -187,8 +190,9 @@ struct PackedArgs {
   TensorArg q, k, v, pk, pv, o;
   PackedPlan plan;
   float* lse;              // nullable
-  float* part_o;           // [slot][key head][row][128]
-  float* part_ml;          // [slot][key head][row][2]: running maximum (log2), sum
+  float* part_o;           // [slot][key head][row of tile][128], then by_row: [key head][row][128]
+  float* part_ml;          // the same with [2]: running maximum (log2), sum
+  int64_t by_row;          // first row of the latter
   int total_q, prefix, Hk, group, causal, pooled;
   uint32_t group_mul, group_shift;   // x / group = x * group_mul >> group_shift for 0 <= x < 2^31
   int max_items;

@@ -73,7 +73,8 @@ __device__ inline bool packed_slot(int Hk, int max_items, int* head, int* item) 
   }
   return *item < max_items;
 }
-inline dim3 packed_grid(int Hk, int max_items) {
+inline dim3 packed_grid(int Hk, int64_t items) {
+  const unsigned max_items = (unsigned)items;
   const int rounds = Hk / kNumXcd, rest = Hk % kNumXcd;
   return dim3(rounds ? kNumXcd * max_items : rest * max_items, rounds + (rest > 0));
 }
@@ -438,8 +439,10 @@ void packed_attn_kernel(PackedArgs a) {
   const int left = it.rows - it.row0 - wave * 32;   // rows of this wave
   // Results go through LDS, so that each store writes whole rows: written from the accumulators, 16 bytes of each
   // of 32 rows at a time, 25,600 x 24 rows without keys took 98 us.
-  if (it.slot >= 0) {
-    const int64_t at = ((int64_t)it.slot * a.Hk + hk) * kTile + wave * 32;
+  if (it.slot != kFinished) {
+    const int64_t at = (it.slot == kByRow ? a.by_row + (int64_t)hk * a.total_q * a.group + it.q0 * a.group - header[kPlanFirstRow] + it.row0
+                                          : ((int64_t)it.slot * a.Hk + hk) * kTile) +
+                       wave * 32;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {   // 64 of a row's 128 values fit the wave's 8 KB
 #pragma unroll
@@ -505,6 +508,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
     const int n = jn.pieces + np;
     const int pooled = jn.q0 * a.group - first_row + row;   // among the rows of all sequences
     auto at = [&](int i) {
+      if (jn.slot == kByRow && i < jn.pieces) return a.by_row + (int64_t)hk * a.total_q * a.group + pooled;
       const int64_t slot = i < jn.pieces ? jn.slot + i : pooled / kTile * np + (i - jn.pieces);
       return (slot * a.Hk + hk) * kTile + (i < jn.pieces ? r : pooled % kTile);
     };
@@ -565,7 +569,7 @@ void launch_packed(const PackedConfig& c, const PackedArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((packed_attn_kernel<BF16, false, true>), grid, block, 0, st, a);
   else
     hipLaunchKernelGGL((packed_attn_kernel<BF16, false, false>), grid, block, 0, st, a);
-  const int64_t groups = (int64_t)c.max_joins * a.Hk * (kPackedTile / 8);
+  const int64_t groups = c.max_joins * a.Hk * (kPackedTile / 8);
   hipLaunchKernelGGL((packed_join_kernel<BF16>), dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, a);
 }
 

@@ -8,7 +8,9 @@
 // first (by 64 classes of length), so the last workgroups to start are the shortest.
 //
 // One workgroup: three passes over the tiles (cost, classes, emission) with two block scans, a few microseconds.
-// A plan never exceeds packed_config's bounds: the extra pieces of a cut come to at most C / chunk <= per_head.
+// A plan never exceeds packed_config's bounds: with pieces of at least C / per_head blocks the cuts come to fewer than
+// per_head pieces more than there were tiles, and the tiles that are cut (5 / 4 of a piece or longer) to fewer than
+// per_head.
 #include <algorithm>
 
 #include "chorus_internal.h"
@@ -38,11 +40,16 @@ PackedConfig packed_config(const chorus_packed_shape& s) {
   // The prefix is worth a pass of its own when the sequences' own tiles are mostly empty: then a tile of pooled
   // rows replaces several walks over it.
   c.pooled = s.prefix > 0 && s.n_seqs > 1 && rows < (int64_t)s.n_seqs * tile;
-  c.per_head = (512 + s.kv_heads - 1) / s.kv_heads;
+  // Two workgroups fit a CU.  Single tokens are bound by memory and their join is short, so three pieces for every two
+  // places even out the end: 64 caches of up to 16,384 keys 226 -> 214 us; with full tiles the longer join costs what
+  // that gains (eight prompts behind a prefix 113 + 11 us, 109 + 21).
+  const bool tokens = s.max_q > 0 && s.max_q * (int64_t)group <= 32 && !c.pooled;
+  c.per_head = ((tokens ? 768 : 512) + s.kv_heads - 1) / s.kv_heads;
   const int64_t tiles = rows / tile + s.n_seqs, pooled_tiles = c.pooled ? rows / tile + 1 : 0;
-  c.max_items = (int32_t)(tiles + pooled_tiles + c.per_head);
-  c.max_slots = c.pooled ? c.max_items : 2 * c.per_head;
-  c.max_joins = c.pooled ? (int32_t)tiles : c.per_head;
+  c.max_items = tiles + pooled_tiles + c.per_head;
+  c.max_slots = (c.pooled ? pooled_tiles + c.per_head : 0) + 2 * c.per_head;
+  c.max_joins = c.pooled ? tiles : c.per_head;
+  c.row_slots = c.pooled ? rows : 0;
   uint32_t h = 2166136261u;
   for (const int32_t v : {s.n_seqs, s.total_q, s.total_k, s.prefix, s.q_heads, s.kv_heads, s.causal, s.max_q})
     h = (h ^ (uint32_t)v) * 16777619u + 0x9e3779b9u;
@@ -191,12 +198,14 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
   const Tile mine = tid < n_tiles ? tile_at(a, seq, tid) : Tile{};
   unsigned long long cost = mine.blocks;
   for (int t = tid + threads; t < n_tiles; t += threads) cost += tile_at(a, seq, t).blocks;
-  if (cost) atomicAdd(&cost_s, cost);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) cost += __shfl_xor(cost, d);
+  if ((tid & 63) == 0) atomicAdd(&cost_s, cost);
   __syncthreads();
   cost = cost_s + (unsigned long long)pooled_tiles * prefix_blocks;
   // (the quotient in fp32: which blocks make a piece may be off by one in 2^24)
   const int piece = max((int)min((float)cost / (float)a.per_head + 1.f, (float)(1 << 26)), kMinChunk);
-  const int longest = piece + piece / 2;
+  const int longest = piece + piece / 4;
   auto pieces = [&](int blocks) { return blocks > longest ? (blocks + piece - 1) / piece : 1; };
   const float per_class = (float)kClasses / (float)(longest + 1);
   // first block of piece i of p
@@ -240,20 +249,21 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
       x = base ? tile_at(a, seq, t) : mine;
       p = a.pooled && x.blocks == 0 ? 0 : pieces(x.blocks);
       joined = a.pooled || p > 1;
-      own = joined ? p : 0;
+      own = p > 1 ? p : 0;   // a whole tile of a pooled batch leaves its result by row
     }
     unsigned long long both = (unsigned long long)own << 32 | joined, upto;   // slots and joins in one scan
     both = block_scan(both, Add(), wave_l, &upto) - both;
     const int slot = slots + (int)(both >> 32), join = joins + (int)(uint32_t)both;
     slots += (int)(upto >> 32);
     joins += (int)(uint32_t)upto;
+    const int first_slot = p > 1 ? slot : joined ? kByRow : kFinished;
     if (p) {
       int at = atomicAdd(&class_s[class_of(x.blocks, p)], p);
       for (int i = 0; i < p; ++i, ++at)
         a.plan.items[at] = {x.seq.q0, x.row0, x.rows, cut(x.blocks, p, i), cut(x.blocks, p, i + 1),
-                            x.seq.k0, x.seq.nk, joined ? slot + i : -1};
+                            x.seq.k0, x.seq.nk, first_slot + i};
     }
-    if (joined) a.plan.joins[join] = {x.seq.q0, x.row0, x.rows, slot, p, {0, 0, 0}};
+    if (joined) a.plan.joins[join] = {x.seq.q0, x.row0, x.rows, first_slot, p, {0, 0, 0}};
   }
   if (tid == 0) {
     a.plan.header[kPlanJoins] = joins;
@@ -271,7 +281,7 @@ hipError_t launch_packed_plan(const chorus_packed_shape& s, const PackedConfig& 
   const PlanArgs a = {q_offsets, k_offsets, k_lens,   plan,       s.n_seqs, s.total_q,  s.total_k, s.prefix,
                       s.q_heads / s.kv_heads, s.causal, kPackedTile, c.pooled, c.per_head, c.key};
   // a thread for each sequence and tile, as far as a workgroup goes: few threads pass its barriers sooner
-  const int most = std::max(s.n_seqs + 1, std::min(c.max_items, kMaxThreads));
+  const int most = std::max(s.n_seqs + 1, (int)std::min<int64_t>(c.max_items, kMaxThreads));
   const int threads = std::min((most + 63) / 64 * 64, kMaxThreads);
   if (s.n_seqs <= kNear)
     hipLaunchKernelGGL((packed_plan_kernel<true>), dim3(1), dim3(threads), 0, st, a);
