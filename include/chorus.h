@@ -518,7 +518,7 @@ chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t
  *                 (strides >= 0; pos_stride_b = 0 shares them); any value.
  * q_out, k_out  : as q and k; the same tensor as the input (same pointer and
  *                 strides) for in place, otherwise their spans of memory must
- *                 not overlap.
+ *                 not overlap.  Neither overlaps the other tensor or output.
  * CHORUS_NORM_TOKEN supports up to 128 heads; B * S * heads <= 2^30.
  * ------------------------------------------------------------------------- */
 typedef enum { CHORUS_NORM_NONE = 0, CHORUS_NORM_HEAD = 1, CHORUS_NORM_TOKEN = 2 } chorus_norm;
@@ -573,7 +573,8 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
  * q, out    : [total_q, q_heads, 128], k, v: [total_k, kv_heads, 128], prefix_k,
  *             prefix_v: [prefix, kv_heads, 128]; f16 or bf16 (dtype); stride_b
  *             is not used.  k and v are not read if total_k = 0 (NULL allowed).
- *             out rows of no sequence are left as they were.
+ *             out rows of no sequence are left as they were.  out may be q
+ *             itself (same pointer and strides); it overlaps nothing else.
  * lse       : optional out (NULL to skip), device float32 [q_heads, total_q].
  * workspace : device scratch of chorus_packed_attn_workspace_size(shape) bytes,
  *             256-byte aligned.  One call at a time may use it.

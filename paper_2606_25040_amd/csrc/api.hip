@@ -743,6 +743,8 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
   if ((!same_tensor(q, q_out) && spans_overlap(q, shape->H, q_out, shape->H, shape->B, shape->S)) ||
       (k && ((!same_tensor(k, k_out) && spans_overlap(k, kv_heads, k_out, kv_heads, shape->B, shape->S)))))
     return fail(CHORUS_ERR_INVALID_ARG, "an output overlaps its input without being the same tensor");
+  if (k && (q_out->data == k->data || k_out->data == q->data || q_out->data == k_out->data))
+    return fail(CHORUS_ERR_INVALID_ARG, "an output overlaps the other tensor");
   a.q = targ(q);
   a.q_out = targ(q_out);
   if (k) {
@@ -856,6 +858,9 @@ chorus_status chorus_packed_attn_fwd(chorus_dtype dtype, const chorus_packed_sha
     if (x.needed && x.t->stride_s > INT32_MAX / (2 * kBlock))
       return fail(CHORUS_ERR_UNSUPPORTED, "%s token stride too large for 32-bit offsets in a block", x.name);
   }
+  for (int i = 2; i < 6; ++i)
+    if (all[i].needed && all[i].t->data == out->data)
+      return fail(CHORUS_ERR_INVALID_ARG, "out overlaps %s", all[i].name);
   if (shape->prefix == 0 && (prefix_k || prefix_v)) return fail(CHORUS_ERR_INVALID_ARG, "prefix tensors without a prefix");
   if (!std::isfinite(sm_scale) || !(sm_scale > 0.f))
     return fail(CHORUS_ERR_INVALID_ARG, "sm_scale must be finite and > 0");

@@ -17,7 +17,9 @@
 
 namespace chorus {
 
-// chunk: blocks per piece at least, so that a piece is worth its launch and its share of the join.
+// Blocks of a piece at least.  One query against 16,384 keys, 32 / 8 heads: 33.6 us with 1 or 2, 28.6 with 4, 26.1 with 8
+// (the join grows with the pieces); against 2,048: 17.2, 16.7, 17.8, 20.9; eight sequences of 300, 16 / 4 heads, causal:
+// 32 with 1 or 2, 19.9 with 4 or more.
 constexpr int kMinChunk = 4;
 constexpr int kClasses = 64;
 
@@ -37,9 +39,10 @@ PackedConfig packed_config(const chorus_packed_shape& s) {
   const int group = s.q_heads / s.kv_heads;
   const int64_t rows = (int64_t)s.total_q * group;
   const int tile = kPackedTile;
-  // The prefix is worth a pass of its own when the sequences' own tiles are mostly empty: then a tile of pooled
-  // rows replaces several walks over it.
-  c.pooled = s.prefix > 0 && s.n_seqs > 1 && rows < (int64_t)s.n_seqs * tile;
+  // The prefix is worth a pass of its own when the sequences' own tiles are mostly empty: then a tile of pooled rows
+  // replaces several walks over it.  16 sequences x 8,192 rows of prefix, 32 / 8 heads: 4 rows each 26 us (walked by
+  // each 63), 64 rows 55 (67), 96 rows 85 (74); 64 x 2,048: 24 (55), 66 (61), 84 (69).
+  c.pooled = s.prefix > 0 && s.n_seqs > 1 && 2 * rows <= (int64_t)s.n_seqs * tile;
   // Two workgroups fit a CU.  Single tokens are bound by memory and their join is short, so three pieces for every two
   // places even out the end: 64 caches of up to 16,384 keys 226 -> 214 us; with full tiles the longer join costs what
   // that gains (eight prompts behind a prefix 113 + 11 us, 109 + 21).

@@ -130,6 +130,8 @@ CASES = {  # nq, nk, H, Hk, dtype, causal, prefix, cache
     "prefix_tokens_exact_blocks": ([1] * 9, [64] * 9, 4, 4, BF16, True, 128, False),
     "prefix_without_own_keys": ([1, 3, 2], [0, 0, 1], 3, 1, F16, True, 65, False),
     "prefix_prompts": ([130, 257, 20], [130, 300, 20], 4, 2, BF16, True, 333, False),
+    "prefix_half_tiles": ([16, 15, 1, 30], [16, 15, 60, 30], 8, 2, BF16, True, 500, False),
+    "prefix_pooled_and_cut": ([1, 2, 1], [900, 4000, 3], 6, 2, F16, True, 2500, True),
     "prefix_full": ([40, 1, 0, 99], [40, 17, 3, 0], 2, 2, F16, False, 63, False),
     "prefix_one_sequence": ([3], [30], 8, 1, BF16, True, 2000, False),
     "prefix_more_queries_than_keys": ([200, 4], [20, 1], 2, 1, BF16, True, 70, False),
@@ -168,6 +170,14 @@ def test_scale_argument_and_strided_views():
     c.q, c.k, c.v = (x.contiguous() for x in (b.q, b.k, b.v))
     same = c.run(sm_scale=0.2)
     assert torch.equal(same[0], out) and torch.equal(same[1], got[1])
+
+
+@pytest.mark.parametrize("nq,nk,prefix", [([130, 1, 40], [130, 3000, 40], 0), ([1] * 9, [70] * 9, 300), ([150, 3], [150, 3], 100)])
+def test_results_in_the_place_of_the_queries(nq, nk, prefix):
+    b = Batch(nq, nk, 4, 2, BF16, prefix=prefix)
+    want = b.run()
+    got = b.run(out=b.q)
+    assert got[0] is b.q and torch.equal(b.q, want[0]) and torch.equal(got[1], want[1])
 
 
 def test_prefix_with_strides_of_its_own():

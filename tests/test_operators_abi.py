@@ -67,6 +67,7 @@ def test_norm_rope_refusals(lib):
     assert rope(lib, qo=t(data=FAKE + 512)) == 1                     # overlaps its input, shifted
     assert b"overlap" in lib.chorus_last_error()
     assert rope(lib, qo=t(ss=8 * 128)) == 1                          # or with other strides
+    assert rope(lib, qo=t(data=0x2000000)) == 1 and rope(lib, ko=t()) == 1 and rope(lib, ko=t(data=0x1000000)) == 1
 
 
 def packed(n=2, tq=10, tk=20, prefix=0, H=4, Hk=2, D=128, causal=1, max_q=0):
@@ -89,7 +90,7 @@ def attend(lib, s, q=None, k=..., v=..., pk=None, pv=None, sm=0.088, plan=FAKE, 
     wsb = lib.chorus_packed_attn_workspace_size(by(s)) if ws_bytes is None else ws_bytes
     k = t() if k is ... else k
     v = t() if v is ... else v
-    return lib.chorus_packed_attn_fwd(dtype, by(s), by(q or t()), by(k), by(v), by(pk), by(pv), sm, plan, need, by(out or t()), None,
+    return lib.chorus_packed_attn_fwd(dtype, by(s), by(q or t()), by(k), by(v), by(pk), by(pv), sm, plan, need, by(out or t(data=0x9000000)), None,
                                       ws, wsb, None)
 
 
@@ -117,6 +118,7 @@ def test_packed_attention_refusals(lib):
     assert attend(lib, s, k=None) == 1 and attend(lib, s, v=None) == 1
     assert attend(lib, s, k=t(ss=1 << 30)) == 2
     assert attend(lib, s, out=t(ss=-128)) == 1
+    assert attend(lib, s, out=t()) == 1                              # k's memory
     assert attend(lib, s, pk=t(), pv=t()) == 1                       # a prefix that the shape does not have
     assert attend(lib, packed(prefix=5)) == 1                        # and one that is missing
     assert attend(lib, packed(prefix=5), pk=t()) == 1
