@@ -150,6 +150,7 @@ hipError_t launch_qk_norm_rope(chorus_dtype dt, RopeArgs a, hipStream_t st);
 constexpr int kPackedWaves = 4, kPackedTile = 32 * kPackedWaves;   // query rows of a tile, 32 per wave
 struct PackedConfig {
   int pooled;          // the prefix is a pass of its own over the rows of all sequences
+  int tokens;          // a sequence has a few query rows at most (as far as is known)
   int per_head;        // pieces of one key head that fill the GPU
   int64_t max_items, max_slots, max_joins;   // what a plan can come to
   int64_t row_slots;   // rows of all sequences whose results are kept by row

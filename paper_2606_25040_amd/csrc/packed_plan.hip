@@ -44,10 +44,11 @@ PackedConfig packed_config(const chorus_packed_shape& s) {
   // each 63), 64 rows 55 (67), 96 rows 85 (74); 64 x 2,048: 24 (55), 66 (61), 84 (69).
   c.pooled = s.prefix > 0 && s.n_seqs > 1 && 2 * rows <= (int64_t)s.n_seqs * tile;
   // Two workgroups fit a CU.  Single tokens are bound by memory and their join is short, so three pieces for every two
-  // places even out the end: 64 caches of up to 16,384 keys 226 -> 214 us; with full tiles the longer join costs what
-  // that gains (eight prompts behind a prefix 113 + 11 us, 109 + 21).
-  const bool tokens = s.max_q > 0 && s.max_q * (int64_t)group <= 32 && !c.pooled;
-  c.per_head = ((tokens ? 768 : 512) + s.kv_heads - 1) / s.kv_heads;
+  // places even out the end: 64 caches of up to 16,384 keys 226 -> 214 us.  With full tiles two workgroups of a CU
+  // slow each other down and the join is longer: three pieces for four places (40 heads x 1,024: 38 us, 512 pieces 50,
+  // 256 39; eight prompts behind a prefix, 16 / 4 heads: 109 + 10 us of join, 117 + 12, 131 + 4).
+  c.tokens = s.max_q > 0 && s.max_q * (int64_t)group <= 32;
+  c.per_head = ((c.pooled ? 512 : c.tokens ? 768 : 384) + s.kv_heads - 1) / s.kv_heads;
   const int64_t tiles = rows / tile + s.n_seqs, pooled_tiles = c.pooled ? rows / tile + 1 : 0;
   c.max_items = tiles + pooled_tiles + c.per_head;
   c.max_slots = (c.pooled ? pooled_tiles + c.per_head : 0) + 2 * c.per_head;
@@ -69,7 +70,7 @@ struct PlanArgs {
   const int32_t* k_offsets;
   const int32_t* k_lens;
   PackedPlan plan;
-  int n_seqs, total_q, total_k, prefix, group, causal, tile, pooled, per_head;
+  int n_seqs, total_q, total_k, prefix, group, kv_heads, causal, tile, pooled, tokens, per_head;
   int32_t key;
 };
 
@@ -209,7 +210,14 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
   // (the quotient in fp32: which blocks make a piece may be off by one in 2^24)
   const int piece = max((int)min((float)cost / (float)a.per_head + 1.f, (float)(1 << 26)), kMinChunk);
   const int longest = piece + piece / 4;
-  auto pieces = [&](int blocks) { return blocks > longest ? (blocks + piece - 1) / piece : 1; };
+  // A cut saves blocks - blocks / p blocks of a tile's way and costs its rows a join; with more than half the CUs taken
+  // by whole tiles that is not worth it for 5 blocks (32 / 8 heads x 700 keys: 24 us whole, 29 cut; 40 x 512: 20 - 24,
+  // 26), with fewer it is for any (8 heads x 700 keys, causal: 21 us with every cut, 24 without the short ones).
+  const int worth = a.pooled || a.tokens || (int64_t)n_tiles * a.kv_heads <= 128 ? 1 : 6;
+  auto pieces = [&](int blocks) {
+    const int p = (blocks + piece - 1) / piece;
+    return blocks > longest && blocks - (blocks + p - 1) / p >= worth ? p : 1;
+  };
   const float per_class = (float)kClasses / (float)(longest + 1);
   // first block of piece i of p
   auto cut = [](int blocks, int p, int i) { return blocks / p * i + min(blocks % p, i); };
@@ -282,7 +290,7 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
 hipError_t launch_packed_plan(const chorus_packed_shape& s, const PackedConfig& c, const int32_t* q_offsets,
                               const int32_t* k_offsets, const int32_t* k_lens, const PackedPlan& plan, hipStream_t st) {
   const PlanArgs a = {q_offsets, k_offsets, k_lens,   plan,       s.n_seqs, s.total_q,  s.total_k, s.prefix,
-                      s.q_heads / s.kv_heads, s.causal, kPackedTile, c.pooled, c.per_head, c.key};
+                      s.q_heads / s.kv_heads, s.kv_heads, s.causal, kPackedTile, c.pooled, c.tokens, c.per_head, c.key};
   // a thread for each sequence and tile, as far as a workgroup goes: few threads pass its barriers sooner
   const int most = std::max(s.n_seqs + 1, (int)std::min<int64_t>(c.max_items, kMaxThreads));
   const int threads = std::min((most + 63) / 64 * 64, kMaxThreads);
