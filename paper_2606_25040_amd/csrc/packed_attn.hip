@@ -1,17 +1,28 @@
 // Attention over packed sequences, f16 / bf16: runs the items of a work plan (packed_plan.hip).
 //
-// A workgroup takes one item for one key head: 32 * NW query rows (row = query * group + head in group), a wave 32
-// of them, against a run of key blocks of 64.  Key blocks are numbered [whole prefix blocks | the sequence's own |
-// the prefix' last, partial one], so the blocks that need a mask come last.  Scores are taken transposed,
-// S^T = K Q^T with v_mfma_f32_32x32x16, so a lane holds scores of one query (lanes l and l ^ 32 split the keys) and
-// the online softmax is lane-local but for one half-wave exchange; O^T += V^T P^T with V^T from the row-major tile
-// through ds_read_b64_tr_b16.  Maxima and sums are fp32 in the log2 domain; P is rounded to the input's type for
-// the matrix cores, as O is once at the end; the running maximum moves (and O is rescaled) only when a row's
-// grew by more than 2^8.
+// A workgroup takes one item for one key head: a tile of 128 query rows (row = query * group + head in group, so the
+// heads that share keys share the tile), four waves of 32 rows, against a run of key blocks of 64.  Key blocks are
+// numbered [whole prefix blocks | the sequence's own | the prefix' last, partial one], so the blocks that need a mask
+// come last.  Scores are taken transposed, S^T = K Q^T with v_mfma_f32_32x32x16, so a lane holds scores of one query
+// (lanes l and l ^ 32 split the keys) and the online softmax is lane-local but for one half-wave exchange; O^T += V^T P^T
+// with V^T from the row-major tile through ds_read_b64_tr_b16.  QK^T of block x + 1 is issued beside the softmax of
+// block x; K and V go global -> LDS into two buffers each, requested a whole step ahead, one barrier per step; 64 KB, so
+// two workgroups share a CU.  Q and the results pass through the second buffers, in whole rows.
 //
-// Rows cut into pieces leave (m, l, O) in fp32 in the workspace; packed_join_kernel joins them.
+// Maxima and sums are fp32 in the log2 domain; P is rounded to the input's type for the matrix cores, as O is once at
+// the end; the running maximum moves (and O is rescaled) only when a row's grew by more than 2^8.  Rows cut into pieces
+// leave (m, l, O) in fp32 in the workspace; packed_join_kernel joins them.
+//
+// What bounds it and what it measured (bf16 unless said): one causal sequence of 20,280, 40 / 8 heads, 3.73-3.95 ms,
+// 1,070-1,130 TFLOP/s, like the dense kernel of one length (matrix cores and the clock under that load); five clips of
+// 12 heads in f16 0.84-0.86 ms, 1,010-1,030; ragged prompts, 32 / 8 heads, 0.32-0.33 ms, 880 (each tile's start and
+// masked end); video tokens attending to 20-512 text tokens 0.11-0.12 ms (tiles of 1 to 8 blocks: the start of a
+// workgroup, 2-3 us, and the latency of its first loads); 64 caches of up to 16,384 keys 0.21 ms, 5.4 TB/s.  Measured
+// beside it: eight waves per workgroup 1 % faster on the longest case, 15-50 % slower on short ones; one and two waves
+// 1.4 to 4 times slower; several tiles per workgroup with the next one's first loads behind the last block 10-20 % slower
+// (registers); the masked blocks' QK^T beside the softmax as well 5-25 % slower (registers); the first V and second K
+// tile requested with the first K tile (80 KB of LDS) no faster; the next item's Q prefetched into L2 no faster.
 #include <cfloat>
-#include <type_traits>
 
 #include "attn_common.h"
 
@@ -191,7 +202,8 @@ void packed_attn_kernel(PackedArgs a) {
   // Address of head dim 0 of tile row r (rows past the last: the last) in q or out.
   auto row_at = [&](const TensorArg& t, int r) {
     const int at = min(it.row0 + r, it.rows - 1), token = in_group(a, at);
-    return static_cast<char*>(const_cast<void*>(t.data)) + 2 * ((int64_t)(it.q0 + token) * t.ss + (int64_t)(hk * a.group + at - token * a.group) * t.sh);
+    return static_cast<char*>(const_cast<void*>(t.data)) +
+           2 * ((int64_t)(it.q0 + token) * t.ss + (int64_t)(hk * a.group + at - token * a.group) * t.sh);
   };
   // This wave's part of the second buffers: its Q rows at first, later its results.  Rows of 256 bytes, as K's.
   char* mine_s = (wave & 2 ? v_s[1] : k_s[1]) + (wave & 1) * (kTileBytes / 2);
@@ -307,17 +319,16 @@ void packed_attn_kernel(PackedArgs a) {
       }
     l_run += sum;
   };
-  auto fragment = [&](const char* vt, int t, int hh, int u) {
-    const char* lo = vt + (32 * t + 16 * hh) * 256 + v_lane_off + (((4 * u + v_c0) ^ v_sw) << 4);
-    return T::transposed(lo, lo + 8 * 256);
-  };
   auto pv = [&](const vec8 (&pf)[2][2], const char* vt) {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) o[u] = T::mfma(fragment(vt, t, hh, u), pf[t][hh], o[u]);
+        for (int u = 0; u < 4; ++u) {
+          const char* lo = vt + (32 * t + 16 * hh) * 256 + v_lane_off + (((4 * u + v_c0) ^ v_sw) << 4);
+          o[u] = T::mfma(T::transposed(lo, lo + 8 * 256), pf[t][hh], o[u]);
+        }
   };
 
   if (n > 0) {
@@ -327,6 +338,7 @@ void packed_attn_kernel(PackedArgs a) {
     if (n_full == 0) mask(s0, limit(0));
     mx = row_max(s0);
 
+    // Block x: its softmax beside QK^T of block x + 1, then PV.
     auto fused = [&](int x, int par, f32x16 (&sc)[2], f32x16 (&sn)[2]) {
       CHORUS_WAIT_LDS_TILES();
       __syncthreads();
@@ -438,11 +450,12 @@ void packed_attn_kernel(PackedArgs a) {
   const int r32 = lane2 & 31, hl2 = lane2 >> 5;
   const int left = it.rows - it.row0 - wave * 32;   // rows of this wave
   // Results go through LDS, so that each store writes whole rows: written from the accumulators, 16 bytes of each
-  // of 32 rows at a time, 25,600 x 24 rows without keys took 98 us.
+  // of 32 rows at a time, 25,600 x 24 rows without keys took 98 us, this way 33.
   if (it.slot != kFinished) {
-    const int64_t at = (it.slot == kByRow ? a.by_row + (int64_t)hk * a.total_q * a.group + it.q0 * a.group - header[kPlanFirstRow] + it.row0
-                                          : ((int64_t)it.slot * a.Hk + hk) * kTile) +
-                       wave * 32;
+    const int64_t row0 = it.slot == kByRow ? a.by_row + (int64_t)hk * a.total_q * a.group + it.q0 * a.group -
+                                                 header[kPlanFirstRow] + it.row0
+                                           : ((int64_t)it.slot * a.Hk + hk) * kTile;
+    const int64_t at = row0 + wave * 32;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {   // 64 of a row's 128 values fit the wave's 8 KB
 #pragma unroll

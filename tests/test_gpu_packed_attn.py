@@ -95,7 +95,7 @@ class Batch:
         none = np.isneginf(lse)
         assert np.array_equal(np.isneginf(l), none) and not out.transpose(1, 0, 2)[none].any()
         tl = ds.T + n * 2.0 ** -25 + 2.0 ** -22 * (1 + np.abs(np.where(none, 0, lse)))
-        assert (np.abs(l - lse)[~none] <= tl[~none]).all()
+        assert (np.abs(l[~none] - lse[~none]) <= tl[~none]).all()
 
 
 def near(got, clean, W, rows):
