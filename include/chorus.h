@@ -581,9 +581,9 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
  * Results are bitwise deterministic for given lengths and inputs.  A row's
  * rounding may depend on the other sequences of the batch (how many pieces its
  * keys are cut into), as in chorus_block_sparse_attn_fwd.
- * Supports q_heads a multiple of kv_heads, total_q * q_heads < 2^31, about 8
- * million tiles (total_q * q_heads / kv_heads / 128 + n_seqs, over the smaller
- * of kv_heads and 8) and up to 2^20 sequences.
+ * Supports q_heads a multiple of kv_heads, total_q * q_heads, total_k and prefix
+ * up to 2^30, about 8 million tiles (total_q * q_heads / kv_heads / 128 + n_seqs,
+ * over the smaller of kv_heads and 8) and 2^20 sequences.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t n_seqs;    /* >= 1                                       */

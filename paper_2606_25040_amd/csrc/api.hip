@@ -775,8 +775,10 @@ static chorus_status check_packed_shape(const chorus_packed_shape* s) {
   if (s->D != kHeadDim) return fail(CHORUS_ERR_UNSUPPORTED, "head dim D=%d unsupported (only 128)", s->D);
   if (s->causal != 0 && s->causal != 1) return fail(CHORUS_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (s->n_seqs > (1 << 20)) return fail(CHORUS_ERR_UNSUPPORTED, "more than 2^20 sequences");
-  // a launch holds less than 2^32 threads in one dimension, and 65,535 blocks in the other
-  if ((int64_t)s->total_q * s->q_heads > INT32_MAX || s->kv_heads > 65535 ||
+  // rows and keys are counted in int32 with a tile or block to spare; a launch holds less than 2^32 threads in one
+  // dimension, and 65,535 blocks in the other
+  if (s->total_k > (1 << 30) || s->prefix > (1 << 30)) return fail(CHORUS_ERR_UNSUPPORTED, "more than 2^30 keys");
+  if ((int64_t)s->total_q * s->q_heads > (1 << 30) || s->kv_heads > 65535 ||
       packed_config(*s).max_items * std::min(s->kv_heads, kNumXcd) * 64 * kPackedWaves > INT32_MAX)
     return fail(CHORUS_ERR_UNSUPPORTED, "too many query rows");
   return CHORUS_OK;

@@ -125,6 +125,8 @@ CASES = {  # nq, nk, H, Hk, dtype, causal, prefix, cache
     "long_causal": ([1500], [1500], 2, 1, BF16, True, 0, False),
     "long_full": ([333, 1200], [333, 1200], 1, 1, F16, False, 0, False),
     "heads_beyond_eight": ([150], [150], 11, 11, BF16, True, 0, False),
+    "group_of_forty": ([1, 9, 0, 33], [200, 9, 5, 70], 40, 1, BF16, True, 0, True),
+    "prefix_group_of_forty": ([1, 2, 1, 1], [3, 70, 1, 200], 40, 1, F16, True, 130, True),
     "prefix_of_one": ([1, 2], [1, 5], 4, 2, BF16, True, 1, False),
     "prefix_tokens": ([1] * 40, list(range(1, 41)), 8, 2, F16, True, 1000, True),
     "prefix_tokens_exact_blocks": ([1] * 9, [64] * 9, 4, 4, BF16, True, 128, False),

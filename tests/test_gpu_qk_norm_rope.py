@@ -68,6 +68,8 @@ CASES = [  # B, S, H, Hk, dtype, norm, pairs, adjacent
     (2, 33, 6, 2, F16, "head", None, True),
     (1, 1111, 9, 2, BF16, "token", None, True),
     (1, 4999, 2, 1, F16, "none", (64,), False),
+    (3, 7000, 1, 1, BF16, "token", (64,), True),       # workgroups that take several tokens, across requests
+    (1, 2500, 64, 0, F16, "token", (32, 32), False),
 ]
 
 

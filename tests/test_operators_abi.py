@@ -76,7 +76,8 @@ def packed(n=2, tq=10, tk=20, prefix=0, H=4, Hk=2, D=128, causal=1, max_q=0):
 
 BAD = [(packed(n=0), 1), (packed(tq=-1), 1), (packed(tk=-1), 1), (packed(prefix=-1), 1), (packed(max_q=-1), 1), (packed(H=5), 1),
        (packed(Hk=0), 1), (packed(H=0, Hk=1), 1), (packed(D=64), 2), (packed(causal=2), 1), (packed(n=(1 << 20) + 1), 2),
-       (packed(tq=1 << 30), 2), (packed(H=70000, Hk=70000, tq=1), 2)]
+       (packed(tq=1 << 30), 2), (packed(H=70000, Hk=70000, tq=1), 2), (packed(tk=(1 << 30) + 1), 2),
+       (packed(prefix=(1 << 30) + 1), 2), (packed(tq=1 << 27, H=8, Hk=8, n=1 << 20), 2)]
 
 
 def make_plan(lib, s, qo=FAKE, ko=FAKE, kl=None, plan=FAKE, nbytes=None):
