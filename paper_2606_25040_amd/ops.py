@@ -620,13 +620,22 @@ def _current(*tensors) -> int:
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        on = t.get_device()
+        if on < 0:
             raise ValueError("expected a device tensor")
         if here is None:
             here = torch.cuda.current_device()
-        if t.get_device() != here:
+        if on != here:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
     return torch._C._cuda_getCurrentRawStream(here)
+
+
+def _heads(t: torch.Tensor):
+    """Pointer to a chorus_tensor of a [B, S, H, 128] tensor."""
+    sb, ss, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError("head dim must be contiguous")
+    return ctypes.byref(Tensor(t.data_ptr(), sb, ss, sh))
 
 
 def _writable(t: torch.Tensor, name: str) -> None:
@@ -687,21 +696,19 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None = None, rotary: RotaryA
     elif k_out is not None:
         raise ValueError("k_out without k")
     for w, heads in ((q_weight, H), (k_weight, Hk)):
-        if w is None:
-            continue
-        shapes = ((D,),) if norm == "head" else ((heads, D), (heads * D,))
-        if norm is None or w.dtype != torch.float32 or tuple(w.shape) not in shapes or not w.is_contiguous():
+        if w is not None and (norm is None or w.dtype != torch.float32 or not w.is_contiguous()
+                              or w.numel() != (D if norm == "head" else heads * D)):
             raise ValueError("a weight must be a contiguous float32 tensor, [128] for norm='head', [heads, 128] for 'token'")
     if (rotary is None) != (positions is None):
         raise ValueError("rotary and positions go together")
     axis_stride = batch_stride = 0
     if rotary is not None:
-        if positions.dtype != torch.int32 or positions.dim() not in (2, 3) or positions.shape[0] != len(rotary.pairs) \
-                or positions.shape[-1] != S or (positions.dim() == 3 and positions.shape[1] != B) \
-                or (positions.stride(-1) != 1 and S > 1):
+        dims, strides = positions.shape, positions.stride()
+        if positions.dtype != torch.int32 or dims not in ((len(rotary.pairs), S), (len(rotary.pairs), B, S)) \
+                or (strides[-1] != 1 and S > 1):
             raise ValueError("positions must be int32 [axes, S] or [axes, B, S] with contiguous tokens")
-        axis_stride = positions.stride(0)
-        batch_stride = positions.stride(1) if positions.dim() == 3 else 0
+        axis_stride = strides[0]
+        batch_stride = strides[1] if len(dims) == 3 else 0
     if q_out is None:
         q_out = torch.empty((B, S, H, D), dtype=q.dtype, device=q.device)
     elif q_out.shape != q.shape or q_out.dtype != q.dtype:
@@ -714,11 +721,10 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None = None, rotary: RotaryA
         raise ValueError("k_out must have k's shape and dtype")
     elif k is not None:
         _writable(k_out, "k_out")
-    st = L.chorus_qk_norm_rope(dt, ctypes.byref(_shape(q)), Hk, ctypes.byref(_tensor(q)),
-                               None if k is None else ctypes.byref(_tensor(k)), _NORMS[norm], _ptr(q_weight),
-                               _ptr(k_weight), float(eps), None if rotary is None else ctypes.byref(rotary.c),
-                               _ptr(positions), axis_stride, batch_stride, ctypes.byref(_tensor(q_out)),
-                               None if k is None else ctypes.byref(_tensor(k_out)), stream)
+    st = L.chorus_qk_norm_rope(dt, ctypes.byref(Shape(B, S, H, D)), Hk, _heads(q), None if k is None else _heads(k),
+                               _NORMS[norm], _ptr(q_weight), _ptr(k_weight), float(eps),
+                               None if rotary is None else ctypes.byref(rotary.c), _ptr(positions), axis_stride,
+                               batch_stride, _heads(q_out), None if k is None else _heads(k_out), stream)
     _check(st, "chorus_qk_norm_rope")
     return q_out if k is None else (q_out, k_out)
 
@@ -730,8 +736,11 @@ class PackedPlan:
     shape: PackedShape
 
     def __post_init__(self):
-        self.workspace_bytes = load_library().chorus_packed_attn_workspace_size(ctypes.byref(self.shape))
-        self.plan_bytes = load_library().chorus_packed_plan_bytes(ctypes.byref(self.shape))
+        L, s = load_library(), self.shape
+        self.workspace_bytes = L.chorus_packed_attn_workspace_size(ctypes.byref(s))
+        self.plan_bytes = L.chorus_packed_plan_bytes(ctypes.byref(s))
+        self.q_dims, self.k_dims = (s.total_q, s.q_heads, s.D), (s.total_k, s.kv_heads, s.D)
+        self.prefix_dims = (s.prefix, s.kv_heads, s.D)
 
     def flags(self) -> int:
         """Synchronises; 0, or 1 (q_offsets) | 2 (k_offsets, k_lens) where offsets or lengths had to be clamped."""
@@ -768,10 +777,10 @@ def plan_packed_attn(q_offsets: torch.Tensor, k_offsets: torch.Tensor, total_q: 
     return out
 
 
-def _rows(t: torch.Tensor, rows: int, heads: int, like: torch.Tensor, name: str):
+def _rows(t: torch.Tensor, dims, dtype, name: str):
     """Pointer to a chorus_tensor of a [rows, heads, 128] tensor."""
-    if t.shape != (rows, heads, 128) or t.dtype != like.dtype:
-        raise ValueError(f"{name} must be a {like.dtype} [{rows}, {heads}, 128] tensor")
+    if t.shape != dims or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {dtype} {list(dims)} tensor")
     ss, sh, sd = t.stride()
     if sd != 1:
         raise ValueError("head dim must be contiguous")
@@ -786,23 +795,25 @@ def packed_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Pac
     total_q]`` fp32 when ``return_lse``); rows of no sequence are not written."""
     L = load_library()
     stream = _current(q, k, v, prefix_k, prefix_v, out, plan.data)
-    s = plan.shape
+    s, dtype = plan.shape, q.dtype
     dt = _dtype_code(q)
     if (prefix_k is None) != (s.prefix == 0) or (prefix_v is None) != (s.prefix == 0):
         raise ValueError(f"the plan's prefix has {s.prefix} rows")
-    ct = [_rows(q, s.total_q, s.q_heads, q, "q"), _rows(k, s.total_k, s.kv_heads, q, "k"),
-          _rows(v, s.total_k, s.kv_heads, q, "v"), None, None]
-    if s.prefix:
-        ct[3:] = _rows(prefix_k, s.prefix, s.kv_heads, q, "prefix_k"), _rows(prefix_v, s.prefix, s.kv_heads, q, "prefix_v")
+    cq = _rows(q, plan.q_dims, dtype, "q")
+    ck, cv = _rows(k, plan.k_dims, dtype, "k"), _rows(v, plan.k_dims, dtype, "v")
+    cpk = cpv = None
+    if prefix_k is not None:
+        cpk = _rows(prefix_k, plan.prefix_dims, dtype, "prefix_k")
+        cpv = _rows(prefix_v, plan.prefix_dims, dtype, "prefix_v")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(plan.q_dims, dtype=dtype, device=q.device)
     else:
         _writable(out, "out")
+    co = _rows(out, plan.q_dims, dtype, "out")
     lse = torch.empty((s.q_heads, s.total_q), dtype=torch.float32, device=q.device) if return_lse else None
     sm = 128 ** -0.5 if sm_scale is None else float(sm_scale)
     ws = _workspace(plan.workspace_bytes, q.device)
-    st = L.chorus_packed_attn_fwd(dt, ctypes.byref(s), *ct, sm, _aligned(plan.data), plan.plan_bytes,
-                                  _rows(out, s.total_q, s.q_heads, q, "out"), _ptr(lse), _aligned(ws),
-                                  plan.workspace_bytes, stream)
+    st = L.chorus_packed_attn_fwd(dt, ctypes.byref(s), cq, ck, cv, cpk, cpv, sm, _aligned(plan.data), plan.plan_bytes, co,
+                                  _ptr(lse), _aligned(ws), plan.workspace_bytes, stream)
     _check(st, "chorus_packed_attn_fwd")
     return (out, lse) if return_lse else out
