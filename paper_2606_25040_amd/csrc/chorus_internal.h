@@ -159,7 +159,8 @@ struct PackedConfig {
 PackedConfig packed_config(const chorus_packed_shape& s);
 
 // Plan buffer (int32): header, one PackedSeq per sequence and one behind, items, joins.
-constexpr int kPlanItems = 0, kPlanJoins = 1, kPlanFlags = 2, kPlanKey = 3, kPlanPrefixPieces = 4, kPlanFirstRow = 5;
+constexpr int kPlanItems = 0, kPlanJoins = 1, kPlanFlags = 2, kPlanKey = 3, kPlanPrefixPieces = 4, kPlanFirstRow = 5,
+              kPlanJoinRows = 6;   // of the tile with most that is joined
 constexpr int kPlanHeader = 16;
 struct PackedSeq {     // rows of q from q0 (to the next one's), first tile, key rows
   int32_t q0, tile0, k0, nk;

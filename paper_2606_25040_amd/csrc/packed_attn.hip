@@ -505,14 +505,14 @@ void packed_attn_kernel(PackedArgs a) {
 template <bool BF16>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   using scalar = typename Type<BF16>::scalar;
-  constexpr int kTile = kPackedTile, kGroups = kTile / 8;
+  constexpr int kTile = kPackedTile;
   const int* header = a.plan.header;
   if (header[kPlanKey] != a.key) return;
   const int np = header[kPlanPrefixPieces], first_row = header[kPlanFirstRow];
-  // the first rows of every tile first: the tiles of single tokens have no others
   const int64_t tiles = (int64_t)header[kPlanJoins] * a.Hk;
+  const int64_t units = tiles * ((header[kPlanJoinRows] + 7) / 8);   // eight rows of a tile each
   const int lane = threadIdx.x & 31;
-  for (int64_t w = blockIdx.x; w < tiles * kGroups; w += gridDim.x) {
+  for (int64_t w = blockIdx.x; w < units; w += gridDim.x) {
     const int r = (int)(w / tiles) * 8 + (threadIdx.x >> 5);
     const int hk = (int)(w % a.Hk);
     const PackedJoin jn = a.plan.joins[w % tiles / a.Hk];

@@ -11,7 +11,7 @@
 // a head, bound by its barriers and the latency of a few dependent loads.
 // A plan never exceeds packed_config's bounds: with pieces of at least C / per_head blocks the cuts come to fewer than
 // per_head pieces more than there were tiles, and the tiles that are cut (5 / 4 of a piece or longer) to fewer than
-// per_head.
+// per_head; a pooled prefix comes to one piece for each of its tiles or to kPrefixPlaces / key heads.
 #include <algorithm>
 
 #include "chorus_internal.h"
@@ -22,6 +22,10 @@ namespace chorus {
 // (the join grows with the pieces); against 2,048: 17.2, 16.7, 17.8, 20.9; eight sequences of 300, 16 / 4 heads, causal:
 // 32 with 1 or 2, 19.9 with 4 or more.
 constexpr int kMinChunk = 4;
+// Pieces of a pooled prefix, over all tiles and key heads at most: one for each CU, as long as the short tiles of the
+// sequences' own keys come beside them (96 single tokens behind 16,384 keys, 32 / 8 heads: 57 us, cut by C / per_head as
+// the others 60-62; 64 behind 30,000, 40 / 8 heads: 70, 73).
+constexpr int kPrefixPlaces = 256;
 constexpr int kClasses = 64;
 
 PackedPlan carve_packed_plan(void* plan, int n_seqs, const PackedConfig& c, size_t* bytes) {
@@ -49,10 +53,11 @@ PackedConfig packed_config(const chorus_packed_shape& s) {
   // slow each other down and the join is longer: three pieces for four places (40 heads x 1,024: 38 us, 512 pieces 50,
   // 256 39; eight prompts behind a prefix, 16 / 4 heads: 109 + 10 us of join, 117 + 12, 131 + 4).
   c.tokens = s.max_q > 0 && s.max_q * (int64_t)group <= 32;
-  c.per_head = ((c.pooled ? 512 : c.tokens ? 768 : 384) + s.kv_heads - 1) / s.kv_heads;
+  c.per_head = ((c.tokens && !c.pooled ? 768 : 384) + s.kv_heads - 1) / s.kv_heads;
   const int64_t tiles = rows / tile + s.n_seqs, pooled_tiles = c.pooled ? rows / tile + 1 : 0;
-  c.max_items = tiles + pooled_tiles + c.per_head;
-  c.max_slots = (c.pooled ? pooled_tiles + c.per_head : 0) + 2 * c.per_head;
+  const int64_t prefix_cuts = c.pooled ? kPrefixPlaces / s.kv_heads : 0;
+  c.max_items = tiles + pooled_tiles + prefix_cuts + c.per_head;
+  c.max_slots = pooled_tiles + prefix_cuts + 2 * c.per_head;
   c.max_joins = c.pooled ? tiles : c.per_head;
   c.row_slots = c.pooled ? rows : 0;
   uint32_t h = 2166136261u;
@@ -140,7 +145,7 @@ template <bool NEAR>
 __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
   __shared__ int wave_s[kMaxThreads / 64];
   __shared__ unsigned long long cost_s, wave_l[kMaxThreads / 64];
-  __shared__ int flags_s, class_s[kClasses];
+  __shared__ int flags_s, join_rows_s, class_s[kClasses];
   __shared__ PackedSeq near_s[NEAR ? kNear + 1 : 1];
   PackedSeq* far = a.plan.seqs;
   auto seqs = [&]() -> auto& {
@@ -154,6 +159,7 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
   if (tid == 0) {
     cost_s = 0;
     flags_s = 0;
+    join_rows_s = 0;
   }
   if (tid < kClasses) class_s[tid] = 0;
   // key rows first: their loads are in flight during the first scan
@@ -225,7 +231,8 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
   auto class_of = [&](int blocks, int p) {
     return kClasses - 1 - min((int)((float)((blocks + p - 1) / p) * per_class), kClasses - 1);
   };
-  const int np = pooled_tiles ? pieces(prefix_blocks) : 0;
+  const int np =
+      pooled_tiles ? max(min(kPrefixPlaces / max(pooled_tiles * a.kv_heads, 1), prefix_blocks / kMinChunk), 1) : 0;
 
   for (int t = tid; t < n_tiles; t += threads) {
     const int n = t < threads ? mine.blocks : tile_at(a, seq, t).blocks, p = pieces(n);
@@ -252,7 +259,7 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
     a.plan.items[at] = {first, t * a.tile, pooled_rows, cut(prefix_blocks, np, i),
                         cut(prefix_blocks, np, i + 1), -1, 0, x};
   }
-  int slots = pooled_tiles * np, joins = 0;
+  int slots = pooled_tiles * np, joins = 0, join_rows = 0;
   for (int base = 0; base < n_tiles; base += threads) {
     const int t = base + tid;
     Tile x = {};
@@ -275,9 +282,17 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
         a.plan.items[at] = {x.seq.q0, x.row0, x.rows, cut(x.blocks, p, i), cut(x.blocks, p, i + 1),
                             x.seq.k0, x.seq.nk, first_slot + i};
     }
-    if (joined) a.plan.joins[join] = {x.seq.q0, x.row0, x.rows, first_slot, p, {0, 0, 0}};
+    if (joined) {
+      join_rows = max(join_rows, min(x.rows - x.row0, a.tile));
+      a.plan.joins[join] = {x.seq.q0, x.row0, x.rows, first_slot, p, {0, 0, 0}};
+    }
   }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) join_rows = max(join_rows, __shfl_xor(join_rows, d));
+  if ((tid & 63) == 0) atomicMax(&join_rows_s, join_rows);
+  __syncthreads();
   if (tid == 0) {
+    a.plan.header[kPlanJoinRows] = join_rows_s;
     a.plan.header[kPlanJoins] = joins;
     a.plan.header[kPlanFlags] = flags_s;
     a.plan.header[kPlanKey] = a.key;
