@@ -734,11 +734,12 @@ class PackedPlan:
     """Work plan of a batch of packed sequences (chorus_plan_packed_attn), for every layer of a step."""
     data: torch.Tensor       # uint8; the plan starts at its first 256-byte boundary
     shape: PackedShape
+    plan_bytes: int = 0      # chorus_packed_plan_bytes(shape)
 
     def __post_init__(self):
         L, s = load_library(), self.shape
         self.workspace_bytes = L.chorus_packed_attn_workspace_size(ctypes.byref(s))
-        self.plan_bytes = L.chorus_packed_plan_bytes(ctypes.byref(s))
+        self.plan_bytes = self.plan_bytes or L.chorus_packed_plan_bytes(ctypes.byref(s))
         self.q_dims, self.k_dims = (s.total_q, s.q_heads, s.D), (s.total_k, s.kv_heads, s.D)
         self.prefix_dims = (s.prefix, s.kv_heads, s.D)
 
@@ -768,7 +769,7 @@ def plan_packed_attn(q_offsets: torch.Tensor, k_offsets: torch.Tensor, total_q: 
                         int(max_q))
     if out is None:
         need = L.chorus_packed_plan_bytes(ctypes.byref(shape))
-        out = PackedPlan(torch.empty(need + 256, dtype=torch.uint8, device=q_offsets.device), shape)
+        out = PackedPlan(torch.empty(need + 256, dtype=torch.uint8, device=q_offsets.device), shape, need)
     elif bytes(out.shape) != bytes(shape):
         raise ValueError("out is a plan of another shape")
     st = L.chorus_plan_packed_attn(ctypes.byref(shape), q_offsets.data_ptr(), k_offsets.data_ptr(), _ptr(k_lens),
