@@ -18,7 +18,7 @@
 // 12 heads in f16 0.84-0.86 ms, 1,010-1,030; ragged prompts, 32 / 8 heads, 0.32-0.33 ms, 880 (each tile's start and
 // masked end); video tokens attending to 20-512 text tokens 0.11-0.12 ms (tiles of 1 to 8 blocks: the start of a
 // workgroup, 2-3 us, and the latency of its first loads); 64 caches of up to 16,384 keys 0.21 ms, 5.4 TB/s.  Measured
-// beside it: eight waves per workgroup 1 % faster on the longest case, 15-50 % slower on short ones; one and two waves
+// beside it: eight waves per workgroup 1 % faster on the longest case, 10-50 % slower on short ones; one and two waves
 // 1.4 to 4 times slower; several tiles per workgroup with the next one's first loads behind the last block 10-20 % slower
 // (registers); the masked blocks' QK^T beside the softmax as well 5-25 % slower (registers); the first V and second K
 // tile requested with the first K tile (80 KB of LDS) no faster; the next item's Q prefetched into L2 no faster.
@@ -582,6 +582,8 @@ void launch_packed(const PackedConfig& c, const PackedArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((packed_attn_kernel<BF16, false, true>), grid, block, 0, st, a);
   else
     hipLaunchKernelGGL((packed_attn_kernel<BF16, false, false>), grid, block, 0, st, a);
+  // How many rows there are to join is known on the device alone: 2,048 workgroups go through them (eight prompts behind
+  // a prefix 10 us, with 256, 512 or 1,024 29, 18, 12, with 4,096 10); without any they take 4-5 us, as fewer do.
   const int64_t groups = c.max_joins * a.Hk * (kPackedTile / 8);
   hipLaunchKernelGGL((packed_join_kernel<BF16>), dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, a);
 }
