@@ -223,7 +223,8 @@ def test_shared_and_unordered_key_ranges():
     assert plan.flags() == 0
 
 
-@pytest.mark.parametrize("nq,nk,prefix", [([128, 40], [128, 40], 0), ([1, 1], [70, 5], 0), ([50, 9], [80, 9], 100)])
+@pytest.mark.parametrize("nq,nk,prefix", [([128, 40], [128, 40], 0), ([1, 1], [70, 5], 0), ([50, 9], [80, 9], 100),
+                                          ([40, 9], [200, 9], 0), ([10, 70], [10, 70], 40)])   # the last two: waves without rows
 @pytest.mark.parametrize("what", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_keys_and_values_that_a_row_does_not_see_may_hold_anything(nq, nk, prefix, what, dtype):
@@ -411,3 +412,34 @@ def test_norm_rotation_and_attention_of_a_layer():
     b = Batch(n, n, H, Hk, BF16)
     b.q, b.k, b.v = q, k, v
     b.check(b.run())
+
+
+def test_refusals_of_the_binding():
+    b = Batch([5, 3], [9, 3], 4, 2, F16)
+    plan = b.plan()
+
+    def no(match, **kw):
+        a = dict(q=b.q, k=b.k, v=b.v, plan=plan) | kw
+        with pytest.raises(ValueError, match=match):
+            ops.packed_attn_fwd(**a)
+
+    no("q must be", q=b.q[:7])
+    no("k must be", k=b.k.to(BF16))
+    no("v must be", v=b.v[:, :1])
+    no("prefix has 0 rows", prefix_k=b.k, prefix_v=b.v)
+    no("out must be", out=b.q[:, :2])
+    no("share memory", out=b.q[:1].expand(8, 4, 128))
+    no("contiguous", q=torch.empty(8, 4, 256, dtype=F16, device="cuda")[:, :, ::2])
+    with pytest.raises(TypeError):
+        ops.packed_attn_fwd(b.q.float(), b.k.float(), b.v.float(), plan)
+    with pytest.raises(RuntimeError, match="out overlaps k"):
+        full = Batch([9], [9], 2, 2, F16)
+        ops.packed_attn_fwd(full.q, full.k, full.v, full.plan(), out=full.k)
+    with pytest.raises(ValueError, match="another shape"):
+        ops.plan_packed_attn(ints(b.qo), ints(b.ko), 8, 12, 4, 2, causal=False, out=plan)
+    with pytest.raises(ValueError, match="int32 vector"):
+        ops.plan_packed_attn(ints(b.qo).long(), ints(b.ko), 8, 12, 4, 2)
+    with pytest.raises(ValueError, match="entries"):
+        ops.plan_packed_attn(ints(b.qo), ints(b.ko[:2]), 8, 12, 4, 2)
+    with pytest.raises(RuntimeError, match="multiple"):
+        ops.plan_packed_attn(ints(b.qo), ints(b.ko), 8, 12, 4, 3)

@@ -175,3 +175,27 @@ def test_captured_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_refusals_of_the_binding():
+    q, k, w = draw((2, 5, 4, 128), BF16, 1), draw((2, 5, 2, 128), BF16, 2), weight((128,), 3)
+    rot, pos = ops.RotaryAxes((32, 32)), torch.zeros(2, 5, dtype=torch.int32, device="cuda")
+
+    def no(match, kind=ValueError, **kw):
+        with pytest.raises(kind, match=match):
+            ops.qk_norm_rope(**(dict(q=q, k=k) | kw))
+
+    no("go together", rotary=rot)
+    no("positions must be", rotary=rot, positions=pos.long())
+    no("positions must be", rotary=rot, positions=pos[:1])
+    no("positions must be", rotary=rot, positions=pos[:, :4])
+    no("k must share", k=k[:, :4], rotary=rot, positions=pos)
+    no("k must share", k=k.to(F16), rotary=rot, positions=pos)
+    no("a weight must be", norm="token", q_weight=w, k_weight=w)
+    no("a weight must be", q_weight=w, rotary=rot, positions=pos)
+    no("a weight is given", RuntimeError, norm="head", q_weight=w)
+    no("neither", RuntimeError)
+    no("q_out must have", rotary=rot, positions=pos, q_out=q[:1])
+    no("share memory", rotary=rot, positions=pos, q_out=q[:1].expand(2, 5, 4, 128))
+    no("overlaps", RuntimeError, rotary=rot, positions=pos, k=q, k_out=q.clone(), q_out=q)
+    no("k_out without k", k=None, k_out=k, rotary=rot, positions=pos)
