@@ -185,12 +185,12 @@ void packed_attn_kernel(PackedArgs a) {
         dma16(lds + NW * u * 1024, from, (uint32_t)min(4 * NW * u + r0, rows - 1) * t.ss + c);
     }
   };
-  // V rows past the block's end: zeros, by the wave that loaded them, before the barrier that publishes them (a weight
-  // of 0 on an infinite value would be NaN).
+  // V rows that no row of the tile sees (past the block's end, or keys of later queries): zeros, by the wave that loaded
+  // them, before the barrier that publishes them (a weight of 0 on an infinite value would be NaN).
   auto trim = [&](int x) {
     const int j = it.j0 + x;
     const bool mine = !PREFIX || (j >= pw && j < pw + own);
-    const int rows = (mine ? it.nk : prefix) - (mine ? j - pw : min(j, pw)) * kBlock;
+    const int rows = (mine ? seen_last : prefix) - (mine ? j - pw : min(j, pw)) * kBlock;
     if (rows >= kBlock) return;
     int ln = lane;
     asm volatile("" : "+v"(ln));   // worked out here: kept across the loops the addresses would cost registers

@@ -238,6 +238,20 @@ def test_keys_and_values_that_a_row_does_not_see_may_hold_anything(nq, nk, prefi
     near(got, clean, W, rows)
 
 
+@pytest.mark.parametrize("nq,nk,H,Hk,prefix", [([2], [2], 128, 1, 0), ([3, 1], [70, 5], 256, 2, 0), ([3], [3], 200, 1, 0),
+                                               ([2, 2, 2], [9, 66, 2], 128, 1, 100), ([5], [66], 129, 1, 0)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), float("-inf")])
+def test_unseen_keys_may_hold_anything_where_a_token_fills_a_tile(nq, nk, H, Hk, prefix, what):
+    """With 128 query heads per key head or more, the rows of a tile may all belong to one token and see the same keys,
+    while its last block holds keys of later tokens."""
+    b = Batch(nq, nk, H, Hk, BF16, prefix=prefix)
+    clean, W = b.run(), b.oracle(absolute=True)[0]
+    b.k[b.ko[1] - 1, :, 3] = what      # the last key of sequence 0: seen by its last query alone
+    b.v[b.ko[1] - 1, :, 17] = what
+    got = b.run()
+    near(got, clean, W, [r for r in range(b.qo[-1]) if r != b.qo[1] - 1])
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_values_that_are_not_finite_reach_the_rows_that_see_them(dtype):
     b = Batch([100], [100], 2, 1, dtype)
