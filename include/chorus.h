@@ -579,8 +579,10 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
  * workspace : device scratch of chorus_packed_attn_workspace_size(shape) bytes,
  *             256-byte aligned.  One call at a time may use it.
  * Results are bitwise deterministic for given lengths and inputs.  A row's
- * rounding may depend on the other sequences of the batch (how many pieces its
- * keys are cut into), as in chorus_block_sparse_attn_fwd.
+ * rounding may depend on the lengths of the other sequences of the batch (how
+ * many pieces its keys are cut into), as in chorus_block_sparse_attn_fwd, and
+ * on whether the results of rows near it are finite; where they are, not on
+ * other rows' queries, nor on keys and values that it does not see.
  * Supports q_heads a multiple of kv_heads, total_q * q_heads, total_k and prefix
  * up to 2^30, about 8 million tiles (total_q * q_heads / kv_heads / 128 + n_seqs,
  * over the smaller of kv_heads and 8) and 2^20 sequences.

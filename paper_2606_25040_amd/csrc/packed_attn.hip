@@ -297,9 +297,11 @@ void packed_attn_kernel(PackedArgs a) {
   };
   auto rescale = [&](float mx) {
     const float m_new = fmaxf(m_run, mx * cl2);
-    if (__builtin_amdgcn_ballot_w64(m_new > m_run + kRescaleLog2) != 0) {
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-      m_run = m_new;
+    const bool grew = m_new > m_run + kRescaleLog2;
+    if (__builtin_amdgcn_ballot_w64(grew) != 0) {
+      // each row for itself: moved along with another row of the wave, its weights would round by what that one sees
+      const float alpha = grew ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+      m_run = grew ? m_new : m_run;
       l_run *= alpha;
 #pragma unroll
       for (int u = 0; u < 4; ++u)

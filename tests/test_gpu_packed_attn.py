@@ -252,6 +252,33 @@ def test_unseen_keys_may_hold_anything_where_a_token_fills_a_tile(nq, nk, H, Hk,
     near(got, clean, W, [r for r in range(b.qo[-1]) if r != b.qo[1] - 1])
 
 
+@pytest.mark.parametrize("nq,nk", [([100], [100]), ([40, 9], [200, 9]), ([300, 1], [300, 700])])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_a_row_is_the_same_whatever_others_see(nq, nk, dtype):
+    """The last token of sequence 0, its query, key and value (all finite): no bit of another row changes."""
+    b = Batch(nq, nk, 4, 2, dtype)
+    clean = b.run()
+    last = b.qo[1] - 1
+    b.q[last], b.k[b.ko[1] - 1], b.v[b.ko[1] - 1] = 3.0, 3.0, 50.0
+    got = b.run()
+    rows = [r for r in range(b.qo[-1]) if r != last]
+    assert torch.equal(got[0][rows], clean[0][rows]) and torch.equal(got[1][:, rows], clean[1][:, rows])
+    assert (got[0][last] == 50).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("prefix", [0, 1000])
+def test_a_row_is_the_same_whatever_other_requests_and_heads_ask(prefix, dtype):
+    b = Batch([1] * 40, list(range(180, 220)), 8, 2, dtype, prefix=prefix)
+    clean = b.run()
+    b.q[3, 1] = 8 * (b.pk[900, 0] if prefix else b.k[b.ko[4] - 1, 0])   # one head of one request, along one late key
+    got = b.run()
+    same = torch.ones(40, 8, dtype=torch.bool, device="cuda")
+    same[3, 1] = False
+    assert torch.equal(got[0][same], clean[0][same]) and torch.equal(got[1].t()[same], clean[1].t()[same])
+    assert not torch.equal(got[0][3, 1], clean[0][3, 1])
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_values_that_are_not_finite_reach_the_rows_that_see_them(dtype):
     b = Batch([100], [100], 2, 1, dtype)
