@@ -893,7 +893,7 @@ chorus_status chorus_packed_attn_fwd(chorus_dtype dtype, const chorus_packed_sha
   a.pooled = c.pooled;
   a.max_items = (int)c.max_items;
   a.by_row = c.max_slots * kPackedTile * shape->kv_heads;
-  a.key = c.key;
+  a.key = packed_key(*shape);
   a.sm_scale = sm_scale;
   return from_hip(launch_packed_attn(dtype, c, a, static_cast<hipStream_t>(stream)), "packed_attn");
 }

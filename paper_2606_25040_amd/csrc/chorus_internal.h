@@ -154,14 +154,22 @@ struct PackedConfig {
   int per_head;        // pieces of one key head that fill the GPU
   int64_t max_items, max_slots, max_joins;   // what a plan can come to
   int64_t row_slots;   // rows of all sequences whose results are kept by row
-  int32_t key;         // of the shape, in the plan's header
 };
 PackedConfig packed_config(const chorus_packed_shape& s);
 
 // Plan buffer (int32): header, one PackedSeq per sequence and one behind, items, joins.
-constexpr int kPlanItems = 0, kPlanJoins = 1, kPlanFlags = 2, kPlanKey = 3, kPlanPrefixPieces = 4, kPlanFirstRow = 5,
-              kPlanJoinRows = 6;   // of the tile with most that is joined
+constexpr int kPlanItems = 0, kPlanJoins = 1, kPlanFlags = 2, kPlanPrefixPieces = 3, kPlanFirstRow = 4,
+              kPlanJoinRows = 5,   // of the tile with most that is joined
+              kPlanShape = 8;      // the shape that the plan was made for, field by field
 constexpr int kPlanHeader = 16;
+struct PackedKey {
+  static constexpr int n = 8;
+  int32_t field[n];
+};
+inline PackedKey packed_key(const chorus_packed_shape& s) {
+  return {{s.n_seqs, s.total_q, s.total_k, s.prefix, s.q_heads, s.kv_heads, s.causal, s.max_q}};
+}
+static_assert(kPlanShape + PackedKey::n <= kPlanHeader, "the shape fits the header");
 struct PackedSeq {     // rows of q from q0 (to the next one's), first tile, key rows
   int32_t q0, tile0, k0, nk;
 };
@@ -198,7 +206,7 @@ struct PackedArgs {
   int total_q, prefix, Hk, group, causal, pooled;
   uint32_t group_mul, group_shift;   // x / group = x * group_mul >> group_shift for 0 <= x < 2^31
   int max_items;
-  int32_t key;
+  PackedKey key;
   float sm_scale;
 };
 hipError_t launch_packed_plan(const chorus_packed_shape& s, const PackedConfig& c, const int32_t* q_offsets,

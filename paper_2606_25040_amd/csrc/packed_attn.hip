@@ -90,6 +90,14 @@ inline dim3 packed_grid(int Hk, int64_t items) {
   return dim3(rounds ? kNumXcd * max_items : rest * max_items, rounds + (rest > 0));
 }
 
+// Was the plan made for the shape of this call?  (A larger one's items would reach past this call's tensors.)
+__device__ inline bool plan_fits(const PackedArgs& a, ConstI32* header) {
+  int32_t differ = 0;
+#pragma unroll
+  for (int i = 0; i < PackedKey::n; ++i) differ |= header[kPlanShape + i] ^ a.key.field[i];
+  return differ == 0;
+}
+
 // 16 bytes per lane from an address per lane to LDS (lane-linear at the wave-uniform byte address lds), as dma16.
 __device__ inline void dma16_from(uint32_t lds, const char* from) {
   uint32_t saved;
@@ -135,7 +143,7 @@ void packed_attn_kernel(PackedArgs a) {
   ConstI32* header = as_constant(a.plan.header);
   ConstI32* words = as_constant(reinterpret_cast<const int32_t*>(a.plan.items + index));
   const PackedItem it = {words[0], words[1], words[2], words[3], words[4], words[5], words[6], words[7]};
-  if ((header[kPlanKey] != a.key) | (index >= header[kPlanItems])) return;
+  if (!plan_fits(a, header) | (index >= header[kPlanItems])) return;
   const int nq = in_group(a, it.rows);
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -508,8 +516,8 @@ template <bool BF16>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
   using scalar = typename Type<BF16>::scalar;
   constexpr int kTile = kPackedTile;
-  const int* header = a.plan.header;
-  if (header[kPlanKey] != a.key) return;
+  ConstI32* header = as_constant(a.plan.header);
+  if (!plan_fits(a, header)) return;
   const int np = header[kPlanPrefixPieces], first_row = header[kPlanFirstRow];
   const int64_t tiles = (int64_t)header[kPlanJoins] * a.Hk;
   const int64_t units = tiles * ((header[kPlanJoinRows] + 7) / 8);   // eight rows of a tile each

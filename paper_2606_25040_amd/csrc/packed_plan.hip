@@ -60,10 +60,6 @@ PackedConfig packed_config(const chorus_packed_shape& s) {
   c.max_slots = pooled_tiles + prefix_cuts + 2 * c.per_head;
   c.max_joins = c.pooled ? tiles : c.per_head;
   c.row_slots = c.pooled ? rows : 0;
-  uint32_t h = 2166136261u;
-  for (const int32_t v : {s.n_seqs, s.total_q, s.total_k, s.prefix, s.q_heads, s.kv_heads, s.causal, s.max_q})
-    h = (h ^ (uint32_t)v) * 16777619u + 0x9e3779b9u;
-  c.key = (int32_t)h;
   return c;
 }
 
@@ -77,7 +73,7 @@ struct PlanArgs {
   const int32_t* k_lens;
   PackedPlan plan;
   int n_seqs, total_q, total_k, prefix, group, kv_heads, causal, tile, pooled, tokens, per_head;
-  int32_t key;
+  PackedKey key;
 };
 
 // Inclusive scan over the workgroup (every thread takes part); `total` is the last thread's value.
@@ -160,6 +156,8 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
     cost_s = 0;
     flags_s = 0;
     join_rows_s = 0;
+#pragma unroll
+    for (int i = 0; i < PackedKey::n; ++i) a.plan.header[kPlanShape + i] = a.key.field[i];
   }
   if (tid < kClasses) class_s[tid] = 0;
   // key rows first: their loads are in flight during the first scan
@@ -295,7 +293,6 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
     a.plan.header[kPlanJoinRows] = join_rows_s;
     a.plan.header[kPlanJoins] = joins;
     a.plan.header[kPlanFlags] = flags_s;
-    a.plan.header[kPlanKey] = a.key;
     a.plan.header[kPlanPrefixPieces] = np;
     a.plan.header[kPlanFirstRow] = first * a.group;
   }
@@ -306,7 +303,7 @@ __global__ __launch_bounds__(kMaxThreads) void packed_plan_kernel(PlanArgs a) {
 hipError_t launch_packed_plan(const chorus_packed_shape& s, const PackedConfig& c, const int32_t* q_offsets,
                               const int32_t* k_offsets, const int32_t* k_lens, const PackedPlan& plan, hipStream_t st) {
   const PlanArgs a = {q_offsets, k_offsets, k_lens,   plan,       s.n_seqs, s.total_q,  s.total_k, s.prefix,
-                      s.q_heads / s.kv_heads, s.kv_heads, s.causal, kPackedTile, c.pooled, c.tokens, c.per_head, c.key};
+                      s.q_heads / s.kv_heads, s.kv_heads, s.causal, kPackedTile, c.pooled, c.tokens, c.per_head, packed_key(s)};
   // a thread for each sequence and tile, as far as a workgroup goes: few threads pass its barriers sooner
   const int most = std::max(s.n_seqs + 1, (int)std::min<int64_t>(c.max_items, kMaxThreads));
   const int threads = std::min((most + 63) / 64 * 64, kMaxThreads);

@@ -346,6 +346,30 @@ def test_a_plan_for_another_shape_writes_nothing():
     assert (out == 3).all()
 
 
+def test_a_plan_for_another_shape_writes_nothing_whichever_field_differs():
+    """A larger plan run as a smaller one would address rows that the tensors do not have.  The first pair of shapes has
+    the same 32-bit hash under a common way of mixing the fields."""
+    shapes = [(41, 3876, 171939, 0, 32, 8, 1, 280), (34, 277, 189076, 0, 32, 8, 1, 69)]
+    base = (7, 300, 900, 64, 8, 4, 1, 50)
+    pairs = [shapes] + [[base, base[:i] + (n,) + base[i + 1:]] for i, n in
+                        enumerate((6, 299, 899, 63, 4, 2, 0, 49))]
+    for made, run in pairs:
+        n, tq, tk, prefix, H, Hk, causal, max_q = made
+        qo = ints(np.linspace(0, tq, n + 1).astype(int))
+        plan = ops.plan_packed_attn(qo, ints(np.linspace(0, tk, n + 1).astype(int)), tq, tk, H, Hk, causal=causal, prefix=prefix,
+                                    max_q=max_q)
+        shape = ops.PackedShape(*run[:6], 128, *run[6:])
+        other = ops.PackedPlan(torch.zeros(plan.data.numel() + (1 << 20), dtype=torch.uint8, device="cuda"), shape)
+        at = [ops._aligned(p.data) - p.data.data_ptr() for p in (plan, other)]
+        other.data[at[1]:at[1] + plan.plan_bytes] = plan.data[at[0]:at[0] + plan.plan_bytes]
+        assert other.plan_bytes <= other.data.numel() - 256
+        q, k = (torch.zeros(dims, dtype=BF16, device="cuda") for dims in (other.q_dims, other.k_dims))
+        pk = torch.zeros(other.prefix_dims, dtype=BF16, device="cuda") if run[3] else None
+        out = torch.full_like(q, 3.0)
+        ops.packed_attn_fwd(q, k, k, other, prefix_k=pk, prefix_v=pk, out=out)
+        assert (out == 3).all(), (made, run)
+
+
 def test_deterministic_and_the_plan_can_be_written_again():
     b = Batch([1] * 30 + [300], [int(x) for x in np.linspace(1, 4000, 30)] + [300], 8, 2, BF16, cache=True)
     plan = b.plan()
