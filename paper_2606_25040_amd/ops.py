@@ -740,6 +740,8 @@ class PackedPlan:
         L, s = load_library(), self.shape
         self.workspace_bytes = L.chorus_packed_attn_workspace_size(ctypes.byref(s))
         self.plan_bytes = self.plan_bytes or L.chorus_packed_plan_bytes(ctypes.byref(s))
+        if self.data.numel() * self.data.element_size() < self.plan_bytes + _aligned(self.data) - self.data.data_ptr():
+            raise ValueError(f"data is shorter than the {self.plan_bytes} bytes of a plan of this shape")
         self.q_dims, self.k_dims = (s.total_q, s.q_heads, s.D), (s.total_k, s.kv_heads, s.D)
         self.prefix_dims = (s.prefix, s.kv_heads, s.D)
 

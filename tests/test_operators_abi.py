@@ -146,6 +146,19 @@ def test_python_refuses_host_tensors():
         ops.RotaryAxes((64,), freqs=[1.0] * 63)
 
 
+def test_a_plan_needs_its_whole_buffer(lib):
+    s = packed()
+    need = lib.chorus_packed_plan_bytes(by(s))
+    with pytest.raises(ValueError, match="shorter"):
+        ops.PackedPlan(torch.zeros(need - 1, dtype=torch.uint8), s)
+    data = torch.zeros(need + 256, dtype=torch.uint8)
+    assert ops.PackedPlan(data, s).plan_bytes == need
+    at = ops._aligned(data) - data.data_ptr()
+    assert ops.PackedPlan(data[at:at + need], s).plan_bytes == need
+    with pytest.raises(ValueError, match="shorter"):
+        ops.PackedPlan(data[at + 16:at + 16 + need], s)
+
+
 def test_ladder_of_each_axis():
     r = ops.RotaryAxes((2, 62), theta=100.0)
     assert r.freqs[:3] == (1.0, 100.0 ** -0.5, 1.0) and r.freqs[63] == 100.0 ** (-61 / 62)
