@@ -517,8 +517,10 @@ chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t
  *                 positions[a * pos_stride_axis + b * pos_stride_b + s]
  *                 (strides >= 0; pos_stride_b = 0 shares them); any value.
  * q_out, k_out  : as q and k; the same tensor as the input (same pointer and
- *                 strides) for in place, otherwise their spans of memory must
- *                 not overlap.  Neither overlaps the other tensor or output.
+ *                 strides) for in place, otherwise an output shares no memory
+ *                 with an input or the other output.  (Refused as well: tensors
+ *                 whose spans overlap with different strides between tokens, or
+ *                 between requests, for which that is not worked out.)
  * CHORUS_NORM_TOKEN supports up to 128 heads; B * S * heads <= 2^30.
  * ------------------------------------------------------------------------- */
 typedef enum { CHORUS_NORM_NONE = 0, CHORUS_NORM_HEAD = 1, CHORUS_NORM_TOKEN = 2 } chorus_norm;
@@ -574,7 +576,8 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
  *             prefix_v: [prefix, kv_heads, 128]; f16 or bf16 (dtype); stride_b
  *             is not used.  k and v are not read if total_k = 0 (NULL allowed).
  *             out rows of no sequence are left as they were.  out may be q
- *             itself (same pointer and strides); it overlaps nothing else.
+ *             itself (same pointer and strides); otherwise it shares no memory
+ *             with an input (refused as in chorus_qk_norm_rope).
  * lse       : optional out (NULL to skip), device float32 [q_heads, total_q].
  * workspace : device scratch of chorus_packed_attn_workspace_size(shape) bytes,
  *             256-byte aligned.  One call at a time may use it.

@@ -6,6 +6,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <utility>
 
 #include "chorus_internal.h"
 
@@ -672,17 +673,55 @@ chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t
   return from_hip(launch_compact(bitmap, words, row_ptr, rows, col_idx, s), "compact");
 }
 
-// Do two [B, S, heads, 128] 16-bit tensors share memory (by the spans of their strides)?
-static bool spans_overlap(const chorus_tensor* x, int Hx, const chorus_tensor* y, int Hy, int B, int S) {
-  auto span = [&](const chorus_tensor* t, int H) {
-    return ((int64_t)(B - 1) * t->stride_b + (int64_t)(S - 1) * t->stride_s + (int64_t)(H - 1) * t->stride_h + kHeadDim) * 2;
-  };
-  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x->data), y0 = reinterpret_cast<uintptr_t>(y->data);
-  return x0 < y0 + span(y, Hy) && y0 < x0 + span(x, Hx);
+// The memory of a 16-bit tensor of 128-value rows: its steps that reach anywhere, largest first.  Sums over steps are
+// taken in 128 bits: strides are the caller's.
+struct Extent {
+  typedef __int128 Bytes;
+  const void* data;
+  int n = 0;
+  struct {
+    Bytes stride;
+    int64_t count;
+  } dim[3];
+  Extent(const chorus_tensor* t, int64_t B, int64_t S, int64_t H) : data(t->data) {
+    for (auto d : {std::make_pair(t->stride_b, B), std::make_pair(t->stride_s, S), std::make_pair(t->stride_h, H)}) {
+      if (d.first == 0 || d.second <= 1) continue;
+      int at = n++;
+      for (; at > 0 && dim[at - 1].stride < (Bytes)d.first * 2; --at) dim[at] = dim[at - 1];
+      dim[at].stride = (Bytes)d.first * 2;
+      dim[at].count = d.second;
+    }
+  }
+  // Bytes from the first to behind the last of dims from .. n - 1
+  Bytes span(int from) const {
+    Bytes s = 2 * kHeadDim;
+    for (int i = from; i < n; ++i) s += dim[i].stride * (dim[i].count - 1);
+    return s;
+  }
+};
+
+// Is memory of y's dims from iy, `ahead` bytes behind that of x's dims from ix, apart from it?  Interleaved tensors (views
+// of one fused row, say) step alike in their largest stride: then only what lies within one step counts, with y's first
+// step behind x's and ahead of it.  Tensors that are neither are taken to overlap where their spans do.
+static bool apart(const Extent& x, int ix, const Extent& y, int iy, Extent::Bytes ahead) {
+  const Extent::Bytes wx = x.span(ix), wy = y.span(iy);
+  if (ahead >= wx || ahead + wy <= 0) return true;
+  const Extent::Bytes sx = ix < x.n ? x.dim[ix].stride : 0, sy = iy < y.n ? y.dim[iy].stride : 0, s = std::max(sx, sy);
+  if (s == 0) return false;
+  const int jx = ix + (sx == s), jy = iy + (sy == s);
+  if (x.span(jx) > s || y.span(jy) > s) return false;
+  const Extent::Bytes within = (ahead % s + s) % s;
+  return apart(x, jx, y, jy, within) && apart(x, jx, y, jy, within - s);
 }
 
-static bool same_tensor(const chorus_tensor* x, const chorus_tensor* y) {
-  return x->data == y->data && x->stride_b == y->stride_b && x->stride_s == y->stride_s && x->stride_h == y->stride_h;
+static bool overlap(const Extent& x, const Extent& y) {
+  return !apart(x, 0, y, 0, (Extent::Bytes)reinterpret_cast<uintptr_t>(y.data) - (Extent::Bytes)reinterpret_cast<uintptr_t>(x.data));
+}
+
+// The same rows at the same places (strides of dims of one count for nothing).
+static bool same_tensor(const chorus_tensor* x, const chorus_tensor* y, int64_t B, int64_t S, int64_t H) {
+  return x->data == y->data && (B <= 1 || x->stride_b == y->stride_b) && (S <= 1 || x->stride_s == y->stride_s) &&
+         (H <= 1 || x->stride_h == y->stride_h);
 }
 
 chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape, int32_t kv_heads,
@@ -740,11 +779,17 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
   const int64_t heads = std::max(shape->H, kv_heads);
   if ((int64_t)shape->B * shape->S > (1 << 30) / heads)
     return fail(CHORUS_ERR_UNSUPPORTED, "B * S * heads exceeds 2^30");
-  if ((!same_tensor(q, q_out) && spans_overlap(q, shape->H, q_out, shape->H, shape->B, shape->S)) ||
-      (k && ((!same_tensor(k, k_out) && spans_overlap(k, kv_heads, k_out, kv_heads, shape->B, shape->S)))))
-    return fail(CHORUS_ERR_INVALID_ARG, "an output overlaps its input without being the same tensor");
-  if (k && (q_out->data == k->data || k_out->data == q->data || q_out->data == k_out->data))
-    return fail(CHORUS_ERR_INVALID_ARG, "an output overlaps the other tensor");
+  const int64_t B = shape->B, S = shape->S;
+  const Extent qi(q, B, S, shape->H), qo(q_out, B, S, shape->H);
+  if (!same_tensor(q, q_out, B, S, shape->H) && overlap(qi, qo))
+    return fail(CHORUS_ERR_INVALID_ARG, "q_out overlaps q without being the same tensor");
+  if (k) {
+    const Extent ki(k, B, S, kv_heads), ko(k_out, B, S, kv_heads);
+    if (!same_tensor(k, k_out, B, S, kv_heads) && overlap(ki, ko))
+      return fail(CHORUS_ERR_INVALID_ARG, "k_out overlaps k without being the same tensor");
+    if (overlap(qo, ki) || overlap(ko, qi) || overlap(qo, ko))
+      return fail(CHORUS_ERR_INVALID_ARG, "an output overlaps the other tensor");
+  }
   a.q = targ(q);
   a.q_out = targ(q_out);
   if (k) {
@@ -848,20 +893,24 @@ chorus_status chorus_packed_attn_fwd(chorus_dtype dtype, const chorus_packed_sha
     const chorus_tensor* t;
     const char* name;
     bool needed;
-  } all[] = {{q, "q", true},
-             {out, "out", true},
-             {k, "k", shape->total_k > 0},
-             {v, "v", shape->total_k > 0},
-             {prefix_k, "prefix_k", shape->prefix > 0},
-             {prefix_v, "prefix_v", shape->prefix > 0}};
+    int rows, heads;
+  } all[] = {{q, "q", true, shape->total_q, shape->q_heads},
+             {out, "out", true, shape->total_q, shape->q_heads},
+             {k, "k", shape->total_k > 0, shape->total_k, shape->kv_heads},
+             {v, "v", shape->total_k > 0, shape->total_k, shape->kv_heads},
+             {prefix_k, "prefix_k", shape->prefix > 0, shape->prefix, shape->kv_heads},
+             {prefix_v, "prefix_v", shape->prefix > 0, shape->prefix, shape->kv_heads}};
   for (const auto& x : all) {
     if (x.needed && (st = check_tensor(x.t, x.name, 2))) return st;
     // a key block's rows are addressed with 32-bit byte offsets from its first
     if (x.needed && x.t->stride_s > INT32_MAX / (2 * kBlock))
       return fail(CHORUS_ERR_UNSUPPORTED, "%s token stride too large for 32-bit offsets in a block", x.name);
   }
+  const Extent o(out, 1, shape->total_q, shape->q_heads);
+  if (!same_tensor(q, out, 1, shape->total_q, shape->q_heads) && overlap(o, Extent(q, 1, shape->total_q, shape->q_heads)))
+    return fail(CHORUS_ERR_INVALID_ARG, "out overlaps q without being the same tensor");
   for (int i = 2; i < 6; ++i)
-    if (all[i].needed && all[i].t->data == out->data)
+    if (all[i].needed && overlap(o, Extent(all[i].t, 1, all[i].rows, all[i].heads)))
       return fail(CHORUS_ERR_INVALID_ARG, "out overlaps %s", all[i].name);
   if (shape->prefix == 0 && (prefix_k || prefix_v)) return fail(CHORUS_ERR_INVALID_ARG, "prefix tensors without a prefix");
   if (!std::isfinite(sm_scale) || !(sm_scale > 0.f))

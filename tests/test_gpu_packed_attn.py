@@ -182,6 +182,20 @@ def test_results_in_the_place_of_the_queries(nq, nk, prefix):
     assert got[0] is b.q and torch.equal(b.q, want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_results_beside_the_inputs_in_one_buffer(heads_first):
+    b = Batch([100, 30], [100, 30], 4, 2, BF16)
+    want = b.run()
+    buf = torch.empty((12, 130, 128) if heads_first else (130, 12, 128), dtype=BF16, device="cuda")
+    rows = buf.transpose(0, 1) if heads_first else buf
+    q, k, out, v = rows.split((4, 2, 4, 2), 1)
+    for to, x in ((q, b.q), (k, b.k), (v, b.v)):
+        to.copy_(x)
+    b.q, b.k, b.v = q, k, v
+    got = b.run(out=out)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_prefix_with_strides_of_its_own():
     b = Batch([1] * 5 + [90], [3, 70, 1, 9, 64, 90], 4, 2, F16, prefix=200)
     want = b.run()

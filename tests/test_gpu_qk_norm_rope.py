@@ -132,6 +132,21 @@ def test_strided_views_shared_positions_and_in_place(norm):
     assert got[0] is q and torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(fused[:, :, H + Hk:], rest)
 
 
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_outputs_between_the_inputs_of_one_buffer(heads_first):
+    B, S, H, Hk = 2, 21, 4, 2
+    rot, pos = ops.RotaryAxes((64,)), torch.arange(S, dtype=torch.int32).cuda()[None]
+    shape = (B, 2 * (H + Hk), S, 128) if heads_first else (B, S, 2 * (H + Hk), 128)
+    buf = draw(shape, BF16, 21)
+    rows = buf.transpose(1, 2) if heads_first else buf
+    q, qo, k, ko = rows.split((H, H, Hk, Hk), 2)
+    was = buf.clone().transpose(1, 2) if heads_first else buf.clone()
+    want = ops.qk_norm_rope(q, k, rotary=rot, positions=pos)
+    ops.qk_norm_rope(q, k, rotary=rot, positions=pos, q_out=qo, k_out=ko)
+    assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
+    assert torch.equal(q, was[:, :, :H]) and torch.equal(k, was[:, :, 2 * H:2 * H + Hk])
+
+
 @pytest.mark.parametrize("norm", ["head", "token", None])
 def test_a_token_or_head_that_is_not_finite_stays_alone(norm):
     q = draw((1, 20, 8, 128), F16, 10)

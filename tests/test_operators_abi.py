@@ -2,6 +2,7 @@
 
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
@@ -144,6 +145,97 @@ def test_python_refuses_host_tensors():
             ops.RotaryAxes(bad)
     with pytest.raises(ValueError, match="freqs"):
         ops.RotaryAxes((64,), freqs=[1.0] * 63)
+
+
+ROW = 2 * 128            # bytes of one head of one token
+
+
+def test_packed_outputs_that_share_memory_are_refused(lib):
+    """Told by the workspace check behind: 5 is a call that passed, and nothing is launched either way."""
+    s = packed(tq=10, tk=20, prefix=6, H=4, Hk=2)
+    far = dict(k=t(data=0x2000000), v=t(data=0x3000000), pk=t(data=0x4000000), pv=t(data=0x5000000), ws=None)
+    base = 0x100000
+
+    def status(q=None, out=None, **kw):
+        st = attend(lib, s, q=q or t(data=base), out=out or t(data=0x9000000), **(far | kw))
+        if st == 1:
+            assert b"overlaps" in lib.chorus_last_error()
+        return st
+
+    assert status() == 5 and status(out=t(data=base)) == 5                   # apart; in place
+    assert status(out=t(128, 4 * 128, base)) == 1                            # q transposed, at the same address
+    assert status(q=t(4 * 128, 128, base), out=t(4 * 128, 128, base + ROW)) == 1
+    for shift, st in ((1, 1), (4, 1), (39, 1), (-39, 1), (40, 5), (-40, 5)):   # moved by heads within one buffer
+        assert status(out=t(data=base + shift * ROW)) == st
+    # views of one fused row of 12 heads: q 0 - 3, k 4 - 5, v 6 - 7, out from 8 or from inside another
+    f = dict(q=t(12 * 128, 128, base), k=t(12 * 128, 128, base + 4 * ROW), v=t(12 * 128, 128, base + 6 * ROW))
+    for head, st in ((0, 5), (1, 1), (3, 1), (4, 1), (5, 1), (7, 1), (8, 5), (9, 1), (11, 1)):
+        assert status(out=t(12 * 128, 128, base + head * ROW), **f) == st, head
+    assert status(out=t(12 * 128, 128, base + 12 * 20 * ROW), **f) == 5       # behind all rows
+    # head-major: [heads, rows, 128] buffers of 20 rows a head, k in heads 4 - 5 of it
+    m = dict(q=t(128, 20 * 128, base), k=t(128, 20 * 128, base + 80 * ROW))
+    for row, st in ((0, 5), (5, 1), (10, 5), (75, 1), (80, 1), (120, 5)):
+        assert status(out=t(128, 20 * 128, base + row * ROW), **m) == st, row
+    for name in ("k", "v", "pk", "pv"):
+        rows = 6 if name[0] == "p" else 20
+        last = (rows - 1) * 4 * 128 * 2 + ROW
+        assert status(out=t(data=far[name].data + last)) == 1                # in its last row's second head
+        assert status(out=t(data=far[name].data + last + ROW)) == 5
+    # one token and one head: strides that reach nowhere
+    s = packed(tq=1, tk=1, prefix=1, H=1, Hk=1)
+    assert status(q=t(7 * 128, 5 * 128, base), out=t(128, 128, base)) == 5
+
+
+def test_norm_rope_outputs_that_share_memory_are_refused(lib):
+    base = 0x100000
+
+    def refused(qo, ko, q=t(12 * 128, 128, base, 99 * 12 * 128), k=t(12 * 128, 128, base + 4 * ROW, 99 * 12 * 128)):
+        st = rope(lib, shape=(3, 10, 4, 128), Hk=2, q=q, k=k, qo=qo, ko=ko)
+        return st == 1 and b"overlaps" in lib.chorus_last_error()
+
+    def view(head, token=0, request=0):
+        return t(12 * 128, 128, base + (head + 12 * token + 12 * 99 * request) * ROW, 99 * 12 * 128)
+
+    far = t(data=0x9000000, sb=10 * 512)
+    assert refused(view(1), far) and refused(view(0, 1), far)          # q's own memory, shifted
+    assert refused(view(4), far) and refused(view(2, 9, 2), far)       # k's
+    assert refused(far, view(3)) and refused(far, view(5))             # q's and k's, from k_out
+    assert refused(view(8), view(10)) and refused(view(8), view(11)) and refused(view(7), view(6, 3))   # each other's
+    assert refused(t(128, 512, base, 99 * 12 * 128), far)              # at q's address, other strides
+    # k in a buffer of its own; q_out shifted into it; k_out shifted into q_out
+    k, out = t(2 * 128, 128, 0x700000, 10 * 2 * 128), t(4 * 128, 128, 0xA00000, 10 * 4 * 128)
+    assert refused(t(4 * 128, 128, 0x700000 + ROW, 10 * 4 * 128), far, k=k)
+    assert refused(out, t(4 * 128, 128, 0xA00000 + 3 * ROW, 10 * 4 * 128), k=k)
+    assert refused(far, t(2 * 128, 128, base + 3 * ROW, 10 * 2 * 128), k=k)
+
+
+def test_outputs_are_told_apart_as_by_their_bytes(lib):
+    """Random places, counts and strides, of rows that overlap each other too: what passes shares no byte, and what shares
+    none passes where the strides between tokens and between heads are the same."""
+    def chunks(x, rows, heads):
+        at = x.data // 16 + (np.arange(rows)[:, None] * x.stride_s + np.arange(heads) * x.stride_h).reshape(-1, 1) // 8
+        return set((at + np.arange(16)).ravel().tolist())
+
+    rng = np.random.default_rng(6)
+    passed = exact = 0
+    for _ in range(3000):
+        tq, tk, H, Hk = (int(n) for n in rng.integers(1, 5, 4))
+        alike = rng.random() < 0.6
+        ss, sh = (8 * int(n) for n in rng.choice([0, 1, 15, 16, 17, 32, 48, 64, 80, 128, 160], 2))
+        out = t(ss, sh, 0x100000)
+        if not alike:
+            ss, sh = (8 * int(n) for n in rng.choice([0, 1, 15, 16, 17, 32, 48, 64, 80, 128, 160], 2))
+        k = t(ss, sh, 0x100000 + 16 * int(rng.integers(-300, 300)))
+        st = attend(lib, packed(tq=tq, tk=tk, H=H * Hk, Hk=Hk), q=t(data=0x9000000), k=k, v=t(data=0x8000000), out=out, ws=None)
+        assert st in (1, 5)
+        shared = bool(chunks(out, tq, H * Hk) & chunks(k, tk, Hk))
+        assert not (shared and st == 5), (tq, tk, H, Hk, out.data, out.stride_s, out.stride_h, k.data, k.stride_s, k.stride_h)
+        passed += st == 5
+        inner, outer = sorted((ss, sh))
+        if alike and not shared and inner >= 128 and outer >= inner * max(H * Hk if inner == sh else tq, Hk if inner == sh else tk):
+            exact += 1
+            assert st == 5
+    assert passed > 500 and exact > 100
 
 
 def test_a_plan_needs_its_whole_buffer(lib):
