@@ -503,8 +503,8 @@ chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t
  *      t = position on its axis * freqs[p] radians:
  *      (a, b) -> (a cos t - b sin t, a sin t + b cos t).
  *      A pair with freqs[p] = 0 does not turn.
- * Everything in fp32 (the angle in float64), rounded once to the type of x.
- * Sums of squares are fp32: values above 2^60 overflow them.
+ * Everything in fp32 (the angle in float64), rounded once to the type of x;
+ * where a sum of squares leaves the fp32 range, of scaled values.
  *
  * q, k          : [B, S, heads, 128] f16 or bf16 (dtype); shape->H heads for q,
  *                 kv_heads for k.  k = NULL (then k_out NULL, kv_heads 0) does

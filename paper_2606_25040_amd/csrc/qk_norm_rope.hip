@@ -14,6 +14,8 @@
 //
 // Memory-bound: at 480p 14B (32,760 tokens x 40 + 40 heads, bf16, norm over the token) 249-260 us, 5.2-5.4 TB/s; at
 // 720p 5B (27,280 x 24 + 24, norm per head) 114-122 us, 5.5-5.9 TB/s, the rate of a plain copy.
+#include <cfloat>
+
 #include "chorus_internal.h"
 
 namespace chorus {
@@ -22,6 +24,11 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kPairs = kHeadDim / 2;
 constexpr double kTurnsPerRadian = 0.15915494309189533577;
+// bf16 values reach 2^128 and 2^-133, so their squares leave the fp32 range.  A token or head whose sum of squares
+// overflows is taken times kDown, and one whose sum is so small that squares may have vanished times kUp, and with it
+// eps by the square: any 128 x 128 values then sum to less than 2^126, and the largest square is above 2^-106.  (With
+// eps >= kSmall a mean below it does not count beside eps.)
+constexpr float kDown = 0x1p-72f, kUp = 0x1p+80f, kSmall = 0x1p-100f;
 
 template <bool BF16>
 struct Pack;
@@ -109,27 +116,47 @@ __global__ __launch_bounds__(1024) void qk_norm_rope_kernel(RopeArgs a) {
       x[2 * i] = Pack<BF16>::lo(r[i]);
       x[2 * i + 1] = Pack<BF16>::hi(r[i]);
     }
-    float total = 0.f;
-    if (NORM != CHORUS_NORM_NONE) {
+    auto squares = [&] {   // of the head, or of the wave's heads and for all waves to add
+      float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) total += x[i] * x[i];
-      total = head_sum(total);
+      for (int i = 0; i < 16; ++i) sum += x[i] * x[i];
+      sum = head_sum(sum);
       if (NORM == CHORUS_NORM_TOKEN) {
 #pragma unroll
-        for (int d = 8; d < 64; d *= 2) total += __shfl_xor(total, d);
-        if ((tid & 63) == 0) sums[par][tid >> 6] = total;
+        for (int d = 8; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        if ((tid & 63) == 0) sums[par][tid >> 6] = sum;
       }
-    }
+      return sum;
+    };
+    auto of_all_waves = [&] {
+      float sum = 0.f;
+      for (int i = 0; i < (int)(blockDim.x >> 6); ++i) sum += sums[par][i];
+      return sum;
+    };
+    float total = 0.f;
+    if (NORM != CHORUS_NORM_NONE) total = squares();
     // the other parity's values are read before the next barrier, so one per token is enough
     if (PAIRS || NORM == CHORUS_NORM_TOKEN) __syncthreads();
     if (NORM != CHORUS_NORM_NONE) {
-      float n = kHeadDim;
+      float n = kHeadDim, eps = a.eps;
       if (NORM == CHORUS_NORM_TOKEN) {
-        total = 0.f;
-        for (int i = 0; i < (int)(blockDim.x >> 6); ++i) total += sums[par][i];
+        total = of_all_waves();
         n *= H;
       }
-      const float f = rsqrtf(total / n + a.eps);
+      // the same for all lanes of a head, or of the workgroup
+      if (BF16 && (!(total <= FLT_MAX) || (total < kSmall && eps < kSmall))) {
+        const float scale = total <= FLT_MAX ? kUp : kDown;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= scale;
+        eps = eps * scale * scale;
+        if (NORM == CHORUS_NORM_TOKEN) __syncthreads();   // the sums are read before they are written again
+        total = squares();
+        if (NORM == CHORUS_NORM_TOKEN) {
+          __syncthreads();
+          total = of_all_waves();
+        }
+      }
+      const float f = rsqrtf(total / n + eps);
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] *= f * w[i];
     }

@@ -164,6 +164,24 @@ def test_a_token_or_head_that_is_not_finite_stays_alone(norm):
     assert torch.isnan(b[0, 3, 2]).any() and not torch.isfinite(b[0, 11, 0]).all()
 
 
+@pytest.mark.parametrize("norm,H", [("head", 3), ("token", 40), ("token", 128), ("token", 1)])
+def test_norm_of_values_whose_squares_leave_the_range(norm, H):
+    """Of bf16 values around 2^-115 to 2^122; an ordinary token between them, and eps of the size of the mean."""
+    scales = [120, 64, 61, 58, 55, 0, -40, -52, -60, -75, -80, -115]
+    every = draw((1, len(scales), H, 128), BF16, 13)
+    for s, e in enumerate(scales):
+        every[0, s] *= 2.0 ** e
+    w = weight((128,) if norm == "head" else (H, 128), 14)
+    for eps, rows in ((2.0 ** 120, 6), (2.0 ** -120, 12), (1e-6, 12), (0.0, 12)):   # (results stay above 2^-126)
+        q = every[:, :rows].contiguous()
+        kw = dict(norm=norm, q_weight=w, eps=eps)
+        check(ops.qk_norm_rope(q, **kw), q, None, None, norm, w, float(np.float32(eps)))
+        both = ops.qk_norm_rope(q, q[:, :, :1].clone(), k_weight=w if norm == "head" else w[:1].contiguous(), **kw)
+        assert torch.equal(both[0], ops.qk_norm_rope(q, **kw))
+    rot, pos = ops.RotaryAxes((64,)), torch.arange(len(scales), dtype=torch.int32).cuda()[None]
+    check(ops.qk_norm_rope(q, rotary=rot, positions=pos, norm=norm, q_weight=w, eps=0.0), q, rot, pos, norm, w, 0.0)
+
+
 def test_zero_rows_give_zero():
     q = torch.zeros(1, 3, 2, 128, dtype=BF16, device="cuda")
     assert not ops.qk_norm_rope(q, norm="head", q_weight=weight((128,), 1)).any()
