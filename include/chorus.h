@@ -508,7 +508,7 @@ chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t
  *
  * q, k          : [B, S, heads, 128] f16 or bf16 (dtype); shape->H heads for q,
  *                 kv_heads for k.  k = NULL (then k_out NULL, kv_heads 0) does
- *                 q alone.
+ *                 q alone.  S = 0: nothing is done.
  * q_weight, k_weight : device float32, contiguous, 16-byte aligned; NULL
  *                 exactly for CHORUS_NORM_NONE (and k_weight without k).
  * eps           : >= 0 and finite.

@@ -732,9 +732,12 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
                                   void* stream) {
   g_last_error[0] = 0;
   chorus_status st;
-  if ((st = check_shape(shape))) return st;
+  const bool none = shape && shape->S == 0;   // no tokens
+  const chorus_shape one = none ? chorus_shape{shape->B, 1, shape->H, shape->D} : chorus_shape{};
+  if ((st = check_shape(none ? &one : shape))) return st;
   if (dtype != CHORUS_F16 && dtype != CHORUS_BF16)
     return fail(CHORUS_ERR_UNSUPPORTED, "norm and rotation take f16 or bf16 (dtype %d)", (int)dtype);
+  if (none) return CHORUS_OK;
   if ((st = check_tensor(q, "q", 2))) return st;
   if ((st = check_tensor(q_out, "q_out", 2))) return st;
   if (!k != !k_out || (k ? kv_heads < 1 : kv_heads != 0))

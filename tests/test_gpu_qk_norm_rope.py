@@ -182,6 +182,15 @@ def test_norm_of_values_whose_squares_leave_the_range(norm, H):
     check(ops.qk_norm_rope(q, rotary=rot, positions=pos, norm=norm, q_weight=w, eps=0.0), q, rot, pos, norm, w, 0.0)
 
 
+def test_no_tokens():
+    """As packed attention takes a batch without queries."""
+    q, k = (torch.empty(1, 0, h, 128, dtype=BF16, device="cuda") for h in (4, 2))
+    rot, pos = ops.RotaryAxes((22, 21, 21)), torch.empty(3, 0, dtype=torch.int32, device="cuda")
+    got = ops.qk_norm_rope(q, k, rotary=rot, positions=pos, norm="head", q_weight=weight((128,), 1), k_weight=weight((128,), 2))
+    assert got[0].shape == q.shape and got[1].shape == k.shape
+    assert ops.qk_norm_rope(q, rotary=rot, positions=pos, q_out=q) is q
+
+
 def test_zero_rows_give_zero():
     q = torch.zeros(1, 3, 2, 128, dtype=BF16, device="cuda")
     assert not ops.qk_norm_rope(q, norm="head", q_weight=weight((128,), 1)).any()

@@ -71,6 +71,13 @@ def test_norm_rope_refusals(lib):
     assert rope(lib, qo=t(data=0x2000000)) == 1 and rope(lib, ko=t()) == 1 and rope(lib, ko=t(data=0x1000000)) == 1
 
 
+def test_norm_rope_of_no_tokens(lib):
+    null = t(data=None)
+    assert rope(lib, shape=(2, 0, 4, 128), q=null, k=null, qo=null, ko=null) == 0
+    assert rope(lib, shape=(2, 0, 4, 64)) == 2 and rope(lib, shape=(2, -1, 4, 128)) == 1 and rope(lib, shape=(0, 0, 4, 128)) == 1
+    assert rope(lib, shape=(2, 0, 4, 128), dtype=ops.FP8_E4M3) == 2
+
+
 def packed(n=2, tq=10, tk=20, prefix=0, H=4, Hk=2, D=128, causal=1, max_q=0):
     return ops.PackedShape(n, tq, tk, prefix, H, Hk, D, causal, max_q)
 
