@@ -521,7 +521,7 @@ chorus_status chorus_visit_refresh(const chorus_block_mask* mask, const uint32_t
  *                 with an input or the other output.  (Refused as well: tensors
  *                 whose spans overlap with different strides between tokens, or
  *                 between requests, for which that is not worked out.)
- * CHORUS_NORM_TOKEN supports up to 128 heads; B * S * heads <= 2^30.
+ * Supports up to 2^22 heads (CHORUS_NORM_TOKEN: 128), B * S * heads <= 2^30.
  * ------------------------------------------------------------------------- */
 typedef enum { CHORUS_NORM_NONE = 0, CHORUS_NORM_HEAD = 1, CHORUS_NORM_TOKEN = 2 } chorus_norm;
 

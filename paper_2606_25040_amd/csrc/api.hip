@@ -780,6 +780,7 @@ chorus_status chorus_qk_norm_rope(chorus_dtype dtype, const chorus_shape* shape,
     a.adjacent = rotary->adjacent;
   }
   const int64_t heads = std::max(shape->H, kv_heads);
+  if (heads > (1 << 22)) return fail(CHORUS_ERR_UNSUPPORTED, "more than 2^22 heads");   // a launch holds 65,535 x 128
   if ((int64_t)shape->B * shape->S > (1 << 30) / heads)
     return fail(CHORUS_ERR_UNSUPPORTED, "B * S * heads exceeds 2^30");
   const int64_t B = shape->B, S = shape->S;

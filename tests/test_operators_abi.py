@@ -71,6 +71,12 @@ def test_norm_rope_refusals(lib):
     assert rope(lib, qo=t(data=0x2000000)) == 1 and rope(lib, ko=t()) == 1 and rope(lib, ko=t(data=0x1000000)) == 1
 
 
+def test_norm_rope_refuses_more_heads_than_a_launch_holds(lib):
+    far = dict(qo=t(data=1 << 40), ko=t(data=1 << 44))
+    assert rope(lib, shape=(1, 1, (1 << 22) + 1, 128), **far) == 2
+    assert rope(lib, shape=(1, 1, 4, 128), Hk=(1 << 22) + 1, k=t(data=1 << 46), **far) == 2
+
+
 def test_norm_rope_of_no_tokens(lib):
     null = t(data=None)
     assert rope(lib, shape=(2, 0, 4, 128), q=null, k=null, qo=null, ko=null) == 0
