@@ -9,19 +9,22 @@
 // block x; K and V go global -> LDS into two buffers each, requested a whole step ahead, one barrier per step; 64 KB, so
 // two workgroups share a CU.  Q and the results pass through the second buffers, in whole rows.
 //
-// Maxima and sums are fp32 in the log2 domain; P is rounded to the input's type for the matrix cores, as O is once at
-// the end; the running maximum moves (and O is rescaled) only when a row's grew by more than 2^8.  Rows cut into pieces
-// leave (m, l, O) in fp32 in the workspace; packed_join_kernel joins them.
+// Maxima and sums are fp32 in the log2 domain; a row's running maximum moves (and its O is rescaled) only when it grew by
+// more than 2^8.  P is rounded to the input's type, as the matrix cores take both factors in 16 bits: half a step for
+// each weight, and an error against float64 1.2 to 1.4 times that of a form that rounds O alone; their sum takes the
+// weights before the rounding.  O is rounded once at the end.  Rows cut into pieces leave (m, l, O) in fp32 in the
+// workspace; packed_join_kernel joins them.
 //
-// What bounds it and what it measured (bf16 unless said): one causal sequence of 20,280, 40 / 8 heads, 3.73-3.95 ms,
-// 1,070-1,130 TFLOP/s, like the dense kernel of one length (matrix cores and the clock under that load); five clips of
-// 12 heads in f16 0.84-0.86 ms, 1,010-1,030; ragged prompts, 32 / 8 heads, 0.32-0.33 ms, 880 (each tile's start and
-// masked end); video tokens attending to 20-512 text tokens 0.11-0.12 ms (tiles of 1 to 8 blocks: the start of a
-// workgroup, 2-3 us, and the latency of its first loads); 64 caches of up to 16,384 keys 0.21 ms, 5.4 TB/s.  Measured
-// beside it: eight waves per workgroup 1 % faster on the longest case, 10-50 % slower on short ones; one and two waves
-// 1.4 to 4 times slower; several tiles per workgroup with the next one's first loads behind the last block 10-20 % slower
-// (registers); the masked blocks' QK^T beside the softmax as well 5-25 % slower (registers); the first V and second K
-// tile requested with the first K tile (80 KB of LDS) no faster; the next item's Q prefetched into L2 no faster.
+// What bounds it and what it measured (bf16 unless said): one causal sequence of 20,280, 40 / 8 heads, 3.7-4.0 ms,
+// 1,050-1,140 TFLOP/s, like the dense kernel of one length (matrix cores and the clock under that load); five clips of
+// 12 heads in f16 0.83-0.87 ms, 1,000-1,040; ragged prompts, 32 / 8 heads, 0.33-0.34 ms, 840-870 (about 15 blocks a tile,
+// with each tile's start and masked end); video tokens attending to 20-512 text tokens 0.11-0.12 ms (tiles of 1 to 8
+// blocks: the start of a workgroup, 2-3 us, and the latency of its first loads); 64 caches of up to 16,384 keys 0.21-0.22
+// ms, 5.2-5.5 TB/s.  Tried while it was built, on forms that were not kept: eight waves per workgroup 1 % faster on the
+// longest case, 10-50 % slower on short ones; one and two waves 1.4 to 4 times slower; several tiles per workgroup with
+// the next one's first loads behind the last block 10-20 % slower (registers); the masked blocks' QK^T beside the softmax
+// as well 5-25 % slower (registers); the first V and second K tile requested with the first K tile (80 KB of LDS) no
+// faster; the next item's Q prefetched into L2 no faster.
 #include <cfloat>
 
 #include "attn_common.h"

@@ -5,15 +5,15 @@
 //   y = x * rsqrt(mean(x^2) + eps) * w   mean over the head (w [128]) or over the token's H heads (w [H, 128]), or y = x;
 //   pair p = 0 .. 63 of a head, the elements (2p, 2p + 1) or (p, p + 64), turned by the angle
 //   positions[axis(p)] * freqs[p]: (a, b) -> (a cos - b sin, a sin + b cos);
-// and rounded once to x's type.  Angles are taken in float64 and reduced to a part of a turn before the fp32
+// and rounded once to x's type (bf16 values whose squares leave the fp32 range are scaled first).  Angles are taken in float64 and reduced to a part of a turn before the fp32
 // sine and cosine: in fp32 the angle of position 100,000 would be off by 0.004 rad already.
 //
 // A lane holds 16 elements of one head, the 16-byte chunks c and c + 8 (c = lane % 8), which hold both elements
 // of the lane's pairs in either layout; a head is 8 lanes.  A workgroup holds one token's heads (up to 128) of one
 // tensor at a time, its weights in registers.
 //
-// Memory-bound: at 480p 14B (32,760 tokens x 40 + 40 heads, bf16, norm over the token) 249-260 us, 5.2-5.4 TB/s; at
-// 720p 5B (27,280 x 24 + 24, norm per head) 114-122 us, 5.5-5.9 TB/s, the rate of a plain copy.
+// Memory-bound: at 480p 14B (32,760 tokens x 40 + 40 heads, bf16, norm over the token) 249-266 us, 5.0-5.4 TB/s; at
+// 720p 5B (27,280 x 24 + 24, norm per head) 114-123 us, 5.4-5.9 TB/s, the rate of a plain copy.
 #include <cfloat>
 
 #include "chorus_internal.h"
